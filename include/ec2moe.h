@@ -293,6 +293,131 @@ ec2moe_status ec2moe_lowrank_fit(const ec2moe_codec_desc* desc, const void* x, c
                                  const float* omega_v, int32_t iters, void* u, void* v, int32_t* status,
                                  void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* ---------------------------------------------------------------- 8-bit experts
+ * Expert networks with weights and activations in 8-bit floating point (e4m3: 4 exponent and
+ * 3 mantissa bits, largest value 448, no infinity, 0x7f = NaN) and a float32 scale for each
+ * block of 128. A number is the product of its 8-bit value and its block's scale.
+ *   rows (activations): one scale per row and 128 consecutive columns,
+ *                       scale [rows][cols / 128]
+ *   weights:            one scale per 128 rows x 128 columns,
+ *                       scale [ceil(rows / 128)][cols / 128] per matrix
+ * The transpose of a weight matrix has the transposed scales.
+ */
+
+/*
+ * Quantise x [n_mats][rows][cols] (float32 or bfloat16 as x_dtype) to q (same shape, one byte
+ * each) and scale. block_rows 1: a scale per row and 128 columns, scale [n_mats][rows][cols/128].
+ * block_rows 128: a scale per 128 x 128 block of a matrix (the last block of rows may be
+ * short), scale [n_mats][ceil(rows/128)][cols/128].
+ * Per block: amax = max(max |x|, 2^-100), scale = amax / 448, q = e4m3(448 x / amax), the quotient
+ * rounded once to float32 and then to the nearest 8-bit value (ties to even). A block that holds a
+ * NaN or an infinity becomes NaN throughout.
+ *   cols a positive multiple of 128; rows, n_mats >= 0 (0: nothing is launched).
+ */
+ec2moe_status ec2moe_fp8_quantize(const void* x, ec2moe_dtype x_dtype, int32_t n_mats, int32_t rows, int32_t cols,
+                                  int32_t block_rows, void* q, float* scale, hipStream_t stream);
+
+/* Shape of an 8-bit product by row segments. */
+typedef struct {
+    int32_t rows;           /* rows of a and out */
+    int32_t n_groups;       /* weight matrices, 1 to 256 */
+    int32_t n;              /* output columns (rows of a weight matrix), any n >= 1 */
+    int32_t k;              /* contraction width, a multiple of 128 */
+    ec2moe_dtype out_dtype; /* of out (an int-sized enum) */
+} ec2moe_fp8_matmul_desc;
+
+/* Workspace bytes of ec2moe_fp8_matmul (may be 0). */
+ec2moe_status ec2moe_fp8_matmul_workspace_size(const ec2moe_fp8_matmul_desc* desc, size_t* bytes /*[host]*/);
+
+/*
+ * out[p][c] = sum_j a[p][j] b_e[c][j] for every row p of segment e, on the numbers that the
+ * 8-bit values and scales stand for. Products of 8-bit values are exact; a block of 128 is
+ * summed in float32, multiplied by its two scales and added to a float32 sum, rounded once to
+ * out_dtype.
+ *   a [rows][k], a_scale [rows][k/128]; b [n_groups][n][k], b_scale [n_groups][ceil(n/128)][k/128]
+ *   seg_offsets [n_groups+1] int32: group e owns rows [seg[e], seg[e+1]), 0 = seg[0] <= ... <=
+ *   seg[n_groups] <= rows, as from ec2moe_permute; NULL with n_groups == 1: every row.
+ *   out [rows][n]; rows at or behind seg[n_groups] are left as they were.
+ *   ws of ec2moe_fp8_matmul_workspace_size bytes. n * k < 2^32.
+ */
+ec2moe_status ec2moe_fp8_matmul(const ec2moe_fp8_matmul_desc* desc, const void* a, const float* a_scale,
+                                const int32_t* seg_offsets, const void* b, const float* b_scale, void* out, void* ws,
+                                size_t ws_bytes, hipStream_t stream);
+
+/* Workspace bytes of ec2moe_fp8_moe_forward for this descriptor. */
+ec2moe_status ec2moe_fp8_moe_workspace_size(const ec2moe_moe_desc* desc, size_t* bytes /*[host]*/);
+
+/*
+ * ec2moe_moe_forward with 8-bit expert weights: x is quantised by rows, the hidden activations
+ * (silu(gate) * up, or relu(W_in x)) are quantised by rows from their float32 values, both products
+ * are those of ec2moe_fp8_matmul, and the combine is ec2moe_combine.
+ *   x [T][d], y [T][d] out in the descriptor's dtype; topk_idx, topk_w as in ec2moe_moe_forward;
+ *   w_gate_up [M][2H][d] (EC2MOE_EXPERT_RELU: [M][H][d]) with w_gate_up_scale [M][2H/128][d/128]
+ *   ([M][H/128][d/128]); w_down [M][d][H] with w_down_scale [M][d/128][H/128], as from
+ *   ec2moe_fp8_quantize with block_rows 128;
+ *   ws of ec2moe_fp8_moe_workspace_size bytes.
+ */
+ec2moe_status ec2moe_fp8_moe_forward(const ec2moe_moe_desc* desc, const void* x, const int32_t* topk_idx,
+                                     const float* topk_w, const void* w_gate_up, const float* w_gate_up_scale,
+                                     const void* w_down, const float* w_down_scale, void* y, void* ws,
+                                     size_t ws_bytes, hipStream_t stream);
+
+/* ---------------------------------------------------------------- training the router */
+
+/* Workspace bytes of ec2moe_balance_loss for this descriptor (may be 0). */
+ec2moe_status ec2moe_balance_loss_workspace_size(const ec2moe_moe_desc* desc, size_t* bytes /*[host]*/);
+
+/*
+ * Load balance loss of a routed batch with per-expert counts and its gradient:
+ *   counts_i = number of assignments to expert i, f_i = counts_i / (T' k),
+ *   P_i = (1/T') sum_t probs[t][i], loss = coef * M * sum_i f_i P_i,
+ * over the T' valid tokens (f is constant: a count has no gradient). With T' = 0 the loss, the
+ * counts and the gradient are 0.
+ *   probs       [T][M] float32, topk_idx [T][k] int32, as from ec2moe_group_gate
+ *   token_valid [T] bytes or NULL: 0 marks a padding token, whose probs and indices are not used
+ *   counts      [M] int32 out or NULL; loss [1] float32 out
+ *   d_probs     [M] float32 out or NULL: coef * M * f_i / T', the gradient of the loss with
+ *               respect to probs[t][i], the same for every valid token t: the d_balance of
+ *               ec2moe_group_gate_backward
+ * Indices outside [0, M) are not counted. d_model and ffn_hidden of the descriptor are not used.
+ */
+ec2moe_status ec2moe_balance_loss(const ec2moe_moe_desc* desc, const float* probs, const int32_t* topk_idx,
+                                  const uint8_t* token_valid, float coef, int32_t* counts, float* loss,
+                                  float* d_probs, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Gradients of a loss with respect to the outputs of the gate; NULL: no such term. */
+typedef struct {
+    const float* d_topk_w;      /* [T][k]: of topk_w */
+    const float* d_probs;       /* [T][M]: of probs */
+    const float* d_balance;     /* [M]: of the probs of every valid token alike (ec2moe_balance_loss) */
+    const uint8_t* token_valid; /* [T] or NULL: 0 marks a padding token, which gives and gets no gradient */
+} ec2moe_gate_grads;
+
+/* Workspace bytes of ec2moe_group_gate_backward for this descriptor. */
+ec2moe_status ec2moe_gate_backward_workspace_size(const ec2moe_moe_desc* desc, size_t* bytes /*[host]*/);
+
+/*
+ * Backward pass of ec2moe_group_gate_ex: gradients of its inputs from those of its outputs.
+ * With g = probs, P_k = sum of g over group k, dg the gradient of g (d_probs + d_balance, and for
+ * a selected expert its d_topk_w, through the division by the selected sum when
+ * EC2MOE_GATE_RENORMALIZE is set) and A_k = sum of g dg over group k:
+ *   local logits  dl_i = g_i dg_i - (g_i / P_k) A_k,   group logits  du_k = A_k - P_k sum_j A_j,
+ *   d_x = dl W_local + du W_global, d_W_local = dl^T x, d_W_global = du^T x, biases: column sums.
+ * The selection is constant. Non-candidates have g = 0 and get no gradient.
+ *   opts    group sizes as in the forward call, or NULL; its workspace is not used. Gates with
+ *           pruned groups (0 < top_groups < K) return EC2MOE_ERR_UNSUPPORTED: the left-out groups'
+ *           share of the group softmax is not in probs.
+ *   x, w_global, w_local, probs [T][M], topk_idx [T][k] (in [0, M)) of the forward call
+ *   d_x [T][d] out (layer dtype) or NULL; d_w_global [K][d], d_w_local [M][d] float32 out, both or
+ *   neither; d_b_global [K], d_b_local [M] float32 out or NULL. Outputs are overwritten, and are zero
+ *   for T = 0. ws of ec2moe_gate_backward_workspace_size bytes.
+ */
+ec2moe_status ec2moe_group_gate_backward(const ec2moe_moe_desc* desc, const ec2moe_gate_opts* opts,
+                                         const ec2moe_gate_grads* grads, const void* x, const void* w_global,
+                                         const void* w_local, const float* probs, const int32_t* topk_idx, void* d_x,
+                                         float* d_w_global, float* d_b_global, float* d_w_local, float* d_b_local,
+                                         void* ws, size_t ws_bytes, hipStream_t stream);
+
 /* ---------------------------------------------------------------- host planner
  * Producers of the candidate mask and of the end/cloud placement of pipeline tasks, run
  * on the host (no GPU work, no stream). The paper leaves the capability function H, the

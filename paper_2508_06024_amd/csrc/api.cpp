@@ -15,7 +15,9 @@
 #include <string>
 #include <vector>
 
+#include "fp8.h"
 #include "internal.h"
+#include "router.h"
 
 namespace ec2moe {
 namespace {
@@ -96,6 +98,20 @@ ec2moe_status check_moe_desc(const ec2moe_moe_desc* d, bool equal_groups = true)
     REQUIRE(A * std::max(d->d_model, d->ffn_hidden) * eb < (int64_t(1) << 32) &&
                 int64_t(2) * d->ffn_hidden * d->d_model * eb < (int64_t(1) << 32),
             EC2MOE_ERR_UNSUPPORTED, "tensor too large for 32-bit byte offsets");
+    return EC2MOE_OK;
+}
+
+// goff[k] = first expert of group k, from the group sizes or K equal groups
+ec2moe_status group_offsets(const ec2moe_moe_desc* desc, const int32_t* sizes, int32_t (&goff)[161]) {
+    const int M = desc->n_experts, K = desc->n_groups;
+    goff[0] = 0;
+    for (int k = 0; k < K; ++k) {
+        const int mk = sizes ? sizes[k] : M / K;
+        REQUIRE(mk >= 1, EC2MOE_ERR_INVALID_ARGUMENT, "group %d has %d experts", k, mk);
+        goff[k + 1] = goff[k] + mk;
+        REQUIRE(goff[k + 1] <= M, EC2MOE_ERR_INVALID_ARGUMENT, "group sizes exceed n_experts %d", M);
+    }
+    REQUIRE(goff[K] == M, EC2MOE_ERR_INVALID_ARGUMENT, "group sizes sum to %d, not n_experts %d", goff[K], M);
     return EC2MOE_OK;
 }
 
@@ -314,14 +330,7 @@ ec2moe_status ec2moe_group_gate_ex(const ec2moe_moe_desc* desc, const ec2moe_gat
     GateArgs a{};
     a.top_groups = top_groups;
     a.equal_groups = sized ? 0 : 1;
-    a.goff[0] = 0;
-    for (int k = 0; k < K; ++k) {
-        const int mk = sized ? opts->group_sizes[k] : M / K;
-        REQUIRE(mk >= 1, EC2MOE_ERR_INVALID_ARGUMENT, "group %d has %d experts", k, mk);
-        a.goff[k + 1] = a.goff[k] + mk;
-        REQUIRE(a.goff[k + 1] <= M, EC2MOE_ERR_INVALID_ARGUMENT, "group sizes exceed n_experts %d", M);
-    }
-    REQUIRE(a.goff[K] == M, EC2MOE_ERR_INVALID_ARGUMENT, "group sizes sum to %d, not n_experts %d", a.goff[K], M);
+    if (ec2moe_status st = group_offsets(desc, opts ? opts->group_sizes : nullptr, a.goff); st != EC2MOE_OK) return st;
     const int words = (M + 63) / 64;
     int pop = 0;
     for (int i = 0; i < words; ++i) {
@@ -508,6 +517,223 @@ ec2moe_status ec2moe_moe_forward(const ec2moe_moe_desc* desc, const void* x, con
         e = launch_combine(static_cast<DType>(desc->dtype), y_perm, inv_perm, topk_w, desc->n_tokens, desc->top_k,
                            desc->d_model, y, stream);
     return hip_status(e, "moe_forward launch");
+}
+
+// ---------------------------------------------------------------- 8-bit experts
+
+ec2moe_status ec2moe_fp8_quantize(const void* x, ec2moe_dtype x_dtype, int32_t n_mats, int32_t rows, int32_t cols,
+                                  int32_t block_rows, void* q, float* scale, hipStream_t stream) {
+    REQUIRE(x_dtype == EC2MOE_F32 || x_dtype == EC2MOE_BF16, EC2MOE_ERR_INVALID_ARGUMENT, "unknown dtype %d",
+            static_cast<int>(x_dtype));
+    REQUIRE(n_mats >= 0 && rows >= 0 && cols > 0, EC2MOE_ERR_INVALID_ARGUMENT,
+            "n_mats and rows must be >= 0 and cols positive");
+    REQUIRE(block_rows == 1 || block_rows == kFp8Block, EC2MOE_ERR_INVALID_ARGUMENT, "block_rows %d is not 1 or %d",
+            block_rows, kFp8Block);
+    REQUIRE(cols % kFp8Block == 0, EC2MOE_ERR_UNSUPPORTED, "cols %d is not a multiple of %d", cols, kFp8Block);
+    // a launch of fewer than 2^32 threads: a workgroup per 64 row blocks, or per 128 x 128 block
+    const double groups = static_cast<double>(n_mats) * (cols / kFp8Block) *
+                          (block_rows == 1 ? rows / 64.0 : (rows + kFp8Block - 1) / kFp8Block);
+    REQUIRE(groups < 16.0e6, EC2MOE_ERR_UNSUPPORTED, "%d x %d x %d values are too many for one launch", n_mats, rows,
+            cols);
+    if (n_mats == 0 || rows == 0) return ok();
+    REQUIRE_PTR(x); REQUIRE_PTR(q); REQUIRE_PTR(scale);
+    REQUIRE_ALIGNED(x); REQUIRE_ALIGNED(q); REQUIRE_ALIGNED(scale);
+    return hip_status(launch_fp8_quantize(static_cast<DType>(x_dtype), x, n_mats, rows, cols, block_rows, q, scale,
+                                          stream),
+                      "fp8_quantize launch");
+}
+
+namespace {
+
+ec2moe_status check_fp8_desc(const ec2moe_fp8_matmul_desc* d) {
+    REQUIRE(d != nullptr, EC2MOE_ERR_INVALID_ARGUMENT, "desc is NULL");
+    REQUIRE(d->out_dtype == EC2MOE_F32 || d->out_dtype == EC2MOE_BF16, EC2MOE_ERR_INVALID_ARGUMENT, "unknown dtype %d",
+            static_cast<int>(d->out_dtype));
+    REQUIRE(d->rows >= 0, EC2MOE_ERR_INVALID_ARGUMENT, "rows %d < 0", d->rows);
+    REQUIRE(d->n_groups > 0 && d->n > 0 && d->k > 0, EC2MOE_ERR_INVALID_ARGUMENT, "n_groups, n and k must be positive");
+    REQUIRE(d->n_groups <= kMaxExperts, EC2MOE_ERR_UNSUPPORTED, "n_groups %d > %d", d->n_groups, kMaxExperts);
+    REQUIRE(d->k % kFp8Block == 0, EC2MOE_ERR_UNSUPPORTED, "k %d is not a multiple of %d", d->k, kFp8Block);
+    REQUIRE(static_cast<int64_t>(d->n) * d->k < (int64_t(1) << 32), EC2MOE_ERR_UNSUPPORTED,
+            "a weight matrix of %d x %d is too large for 32-bit byte offsets", d->n, d->k);
+    REQUIRE(fp8_gemm_fits(d->rows, d->n_groups, d->n), EC2MOE_ERR_UNSUPPORTED, "%d x %d outputs are too many for one launch",
+            d->rows, d->n);
+    return EC2MOE_OK;
+}
+
+constexpr const char* kFp8MatmulName = "fp8_matmul";  // of the timing record; outside the layer step
+
+struct Fp8MoeWs {
+    size_t counts, seg, perm_src, inv_perm, xq, xs, act, act_q, act_s, y_perm, total;
+};
+
+Fp8MoeWs fp8_moe_ws(const ec2moe_moe_desc* d) {
+    const int64_t T = d->n_tokens, A = T * d->top_k, kb = d->d_model / kFp8Block, hb = d->ffn_hidden / kFp8Block;
+    Fp8MoeWs w{};
+    size_t o = 0;
+    w.counts = o; o += up(static_cast<size_t>(std::max(1, perm_chunks(A))) * d->n_experts * 4);
+    w.seg = o; o += up(static_cast<size_t>(d->n_experts + 1) * 4);
+    w.perm_src = o; o += up(static_cast<size_t>(A) * 4);
+    w.inv_perm = o; o += up(static_cast<size_t>(A) * 4);
+    w.xq = o; o += up(static_cast<size_t>(T) * d->d_model);
+    w.xs = o; o += up(static_cast<size_t>(T) * kb * 4);
+    w.act = o; o += up(static_cast<size_t>(A) * d->ffn_hidden * 4);
+    w.act_q = o; o += up(static_cast<size_t>(A) * d->ffn_hidden);
+    w.act_s = o; o += up(static_cast<size_t>(A) * hb * 4);
+    w.y_perm = o; o += up(static_cast<size_t>(A) * d->d_model * elem_bytes(static_cast<DType>(d->dtype)));
+    w.total = o;
+    return w;
+}
+
+}  // namespace
+
+ec2moe_status ec2moe_fp8_matmul_workspace_size(const ec2moe_fp8_matmul_desc* desc, size_t* bytes) {
+    if (ec2moe_status st = check_fp8_desc(desc); st != EC2MOE_OK) return st;
+    REQUIRE_PTR(bytes);
+    *bytes = 0;
+    return ok();
+}
+
+ec2moe_status ec2moe_fp8_matmul(const ec2moe_fp8_matmul_desc* desc, const void* a, const float* a_scale,
+                                const int32_t* seg_offsets, const void* b, const float* b_scale, void* out, void* ws,
+                                size_t ws_bytes, hipStream_t stream) {
+    if (ec2moe_status st = check_fp8_desc(desc); st != EC2MOE_OK) return st;
+    REQUIRE(seg_offsets != nullptr || desc->n_groups == 1, EC2MOE_ERR_INVALID_ARGUMENT,
+            "seg_offsets is NULL with %d groups", desc->n_groups);
+    if (ec2moe_status st = check_ws(ws, ws_bytes, 0); st != EC2MOE_OK) return st;
+    if (desc->rows == 0) return ok();
+    REQUIRE_PTR(a); REQUIRE_PTR(a_scale); REQUIRE_PTR(b); REQUIRE_PTR(b_scale); REQUIRE_PTR(out);
+    REQUIRE_ALIGNED(a); REQUIRE_ALIGNED(a_scale); REQUIRE_ALIGNED(b); REQUIRE_ALIGNED(b_scale); REQUIRE_ALIGNED(out);
+    Fp8GemmArgs g{};
+    g.a = static_cast<const uint8_t*>(a); g.a_scale = a_scale; g.seg = seg_offsets; g.n_groups = desc->n_groups;
+    g.rows = desc->rows; g.src_rows = desc->rows; g.b = static_cast<const uint8_t*>(b); g.b_scale = b_scale;
+    g.b_rows = desc->n; g.K = desc->k; g.N = desc->n; g.out = out; g.name = kFp8MatmulName;
+    return hip_status(launch_fp8_gemm(Epilogue::Store, static_cast<DType>(desc->out_dtype), g, stream),
+                      "fp8_matmul launch");
+}
+
+ec2moe_status ec2moe_fp8_moe_workspace_size(const ec2moe_moe_desc* desc, size_t* bytes) {
+    if (ec2moe_status st = check_moe_desc(desc, false); st != EC2MOE_OK) return st;
+    REQUIRE_PTR(bytes);
+    *bytes = fp8_moe_ws(desc).total;
+    return ok();
+}
+
+ec2moe_status ec2moe_fp8_moe_forward(const ec2moe_moe_desc* desc, const void* x, const int32_t* topk_idx,
+                                     const float* topk_w, const void* w_gate_up, const float* w_gate_up_scale,
+                                     const void* w_down, const float* w_down_scale, void* y, void* ws,
+                                     size_t ws_bytes, hipStream_t stream) {
+    if (ec2moe_status st = check_moe_desc(desc, false); st != EC2MOE_OK) return st;
+    const Fp8MoeWs w = fp8_moe_ws(desc);
+    if (ec2moe_status st = check_ws(ws, ws_bytes, w.total); st != EC2MOE_OK) return st;
+    if (desc->n_tokens == 0) return ok();
+    REQUIRE_PTR(x); REQUIRE_PTR(topk_idx); REQUIRE_PTR(topk_w); REQUIRE_PTR(w_gate_up); REQUIRE_PTR(w_gate_up_scale);
+    REQUIRE_PTR(w_down); REQUIRE_PTR(w_down_scale); REQUIRE_PTR(y);
+    REQUIRE_ALIGNED(x); REQUIRE_ALIGNED(w_gate_up); REQUIRE_ALIGNED(w_gate_up_scale); REQUIRE_ALIGNED(w_down);
+    REQUIRE_ALIGNED(w_down_scale); REQUIRE_ALIGNED(y);
+    const DType dt = static_cast<DType>(desc->dtype);
+    const int T = desc->n_tokens, d = desc->d_model, H = desc->ffn_hidden, M = desc->n_experts;
+    const int64_t A = static_cast<int64_t>(T) * desc->top_k;
+    const bool relu = (desc->flags & EC2MOE_EXPERT_RELU) != 0;
+    REQUIRE(fp8_gemm_fits(A, M, H) && fp8_gemm_fits(A, M, d), EC2MOE_ERR_UNSUPPORTED,
+            "%lld assignments are too many for one launch", static_cast<long long>(A));
+    int32_t* seg = at<int32_t>(ws, w.seg);
+    int32_t* perm_src = at<int32_t>(ws, w.perm_src);
+    int32_t* inv_perm = at<int32_t>(ws, w.inv_perm);
+    hipError_t e = launch_permute(topk_idx, A, desc->top_k, M, at<int32_t>(ws, w.counts), seg, perm_src, inv_perm,
+                                  stream);
+    if (e == hipSuccess) e = launch_fp8_quantize(dt, x, 1, T, d, 1, at<void>(ws, w.xq), at<float>(ws, w.xs), stream);
+    if (e == hipSuccess) {
+        Fp8GemmArgs g{};
+        g.a = at<uint8_t>(ws, w.xq); g.a_scale = at<float>(ws, w.xs); g.row_index = perm_src; g.seg = seg;
+        g.n_groups = M; g.rows = A; g.src_rows = T; g.b = static_cast<const uint8_t*>(w_gate_up);
+        g.b_scale = w_gate_up_scale; g.b_rows = relu ? H : 2 * H; g.K = d; g.N = H; g.out = at<void>(ws, w.act);
+        g.name = relu ? "fp8_expert_in_relu" : "fp8_expert_gate_up";
+        e = launch_fp8_gemm(relu ? Epilogue::ReLU : Epilogue::SwiGLU, DType::F32, g, stream);
+    }
+    if (e == hipSuccess)
+        e = launch_fp8_quantize(DType::F32, at<void>(ws, w.act), 1, static_cast<int>(A), H, 1, at<void>(ws, w.act_q),
+                                at<float>(ws, w.act_s), stream);
+    if (e == hipSuccess) {
+        Fp8GemmArgs g{};
+        g.a = at<uint8_t>(ws, w.act_q); g.a_scale = at<float>(ws, w.act_s); g.seg = seg; g.n_groups = M; g.rows = A;
+        g.src_rows = A; g.b = static_cast<const uint8_t*>(w_down); g.b_scale = w_down_scale; g.b_rows = d; g.K = H;
+        g.N = d; g.out = at<void>(ws, w.y_perm); g.name = "fp8_expert_down";
+        e = launch_fp8_gemm(Epilogue::Store, dt, g, stream);
+    }
+    if (e == hipSuccess)
+        e = launch_combine(dt, at<void>(ws, w.y_perm), inv_perm, topk_w, T, desc->top_k, d, y, stream);
+    return hip_status(e, "fp8_moe_forward launch");
+}
+
+// ---------------------------------------------------------------- training the router
+
+ec2moe_status ec2moe_balance_loss_workspace_size(const ec2moe_moe_desc* desc, size_t* bytes) {
+    if (ec2moe_status st = check_moe_desc(desc, false); st != EC2MOE_OK) return st;
+    REQUIRE_PTR(bytes);
+    *bytes = balance_ws_bytes(desc->n_tokens, desc->n_experts);
+    return ok();
+}
+
+ec2moe_status ec2moe_balance_loss(const ec2moe_moe_desc* desc, const float* probs, const int32_t* topk_idx,
+                                  const uint8_t* token_valid, float coef, int32_t* counts, float* loss,
+                                  float* d_probs, void* ws, size_t ws_bytes, hipStream_t stream) {
+    if (ec2moe_status st = check_moe_desc(desc, false); st != EC2MOE_OK) return st;
+    if (ec2moe_status st = check_ws(ws, ws_bytes, balance_ws_bytes(desc->n_tokens, desc->n_experts)); st != EC2MOE_OK)
+        return st;
+    REQUIRE_PTR(loss);
+    if (desc->n_tokens > 0) {
+        REQUIRE_PTR(probs); REQUIRE_PTR(topk_idx);
+        REQUIRE_ALIGNED(probs);
+    }
+    BalanceArgs a{};
+    a.probs = probs; a.topk_idx = topk_idx; a.valid = token_valid; a.coef = coef;
+    a.n_tokens = desc->n_tokens; a.n_experts = desc->n_experts; a.top_k = desc->top_k;
+    a.counts = counts; a.loss = loss; a.d_probs = d_probs; a.ws = ws;
+    return hip_status(launch_balance(a, stream), "balance_loss launch");
+}
+
+ec2moe_status ec2moe_gate_backward_workspace_size(const ec2moe_moe_desc* desc, size_t* bytes) {
+    if (ec2moe_status st = check_moe_desc(desc, false); st != EC2MOE_OK) return st;
+    REQUIRE_PTR(bytes);
+    *bytes = gate_backward_ws_bytes(static_cast<DType>(desc->dtype), desc->n_tokens, desc->d_model, desc->n_experts,
+                                    desc->n_groups);
+    return ok();
+}
+
+ec2moe_status ec2moe_group_gate_backward(const ec2moe_moe_desc* desc, const ec2moe_gate_opts* opts,
+                                         const ec2moe_gate_grads* grads, const void* x, const void* w_global,
+                                         const void* w_local, const float* probs, const int32_t* topk_idx, void* d_x,
+                                         float* d_w_global, float* d_b_global, float* d_w_local, float* d_b_local,
+                                         void* ws, size_t ws_bytes, hipStream_t stream) {
+    const bool sized = opts && opts->group_sizes;
+    if (ec2moe_status st = check_moe_desc(desc, !sized); st != EC2MOE_OK) return st;
+    REQUIRE_PTR(grads);
+    const int M = desc->n_experts, K = desc->n_groups, T = desc->n_tokens;
+    const int top_groups = opts ? opts->top_groups : 0;
+    REQUIRE(top_groups >= 0, EC2MOE_ERR_INVALID_ARGUMENT, "top_groups %d < 0", top_groups);
+    REQUIRE(top_groups == 0 || top_groups >= K, EC2MOE_ERR_UNSUPPORTED,
+            "top_groups %d of %d: the gradient needs every group's probabilities", top_groups, K);
+    GateBackwardArgs a{};
+    if (ec2moe_status st = group_offsets(desc, opts ? opts->group_sizes : nullptr, a.goff); st != EC2MOE_OK) return st;
+    const DType dt = static_cast<DType>(desc->dtype);
+    const size_t need = gate_backward_ws_bytes(dt, T, desc->d_model, M, K);
+    if (ec2moe_status st = check_ws(ws, ws_bytes, need); st != EC2MOE_OK) return st;
+    REQUIRE((d_w_global == nullptr) == (d_w_local == nullptr), EC2MOE_ERR_INVALID_ARGUMENT,
+            "d_w_global and d_w_local must both be given or both be NULL");
+    if (T > 0) {
+        REQUIRE_PTR(probs);
+        REQUIRE(!grads->d_topk_w || topk_idx, EC2MOE_ERR_INVALID_ARGUMENT, "topk_idx is NULL");
+        if (d_w_local) { REQUIRE_PTR(x); REQUIRE_ALIGNED(x); }
+        if (d_x) { REQUIRE_PTR(w_global); REQUIRE_PTR(w_local); REQUIRE_ALIGNED(w_global); REQUIRE_ALIGNED(w_local); }
+    }
+    if (d_x) REQUIRE_ALIGNED(d_x);
+    if (d_w_local) { REQUIRE_ALIGNED(d_w_global); REQUIRE_ALIGNED(d_w_local); }
+    a.x = x; a.w_global = w_global; a.w_local = w_local; a.probs = probs; a.topk_idx = topk_idx;
+    a.d_topk_w = grads->d_topk_w; a.d_probs = grads->d_probs; a.d_balance = grads->d_balance;
+    a.valid = grads->token_valid; a.d_x = d_x; a.d_w_global = d_w_global; a.d_w_local = d_w_local;
+    a.d_b_global = d_b_global; a.d_b_local = d_b_local; a.n_tokens = T; a.d = desc->d_model; a.n_experts = M;
+    a.n_groups = K; a.top_k = desc->top_k; a.renormalize = (desc->flags & EC2MOE_GATE_RENORMALIZE) != 0; a.ws = ws;
+    return hip_status(launch_gate_backward(dt, a, stream), "group_gate_backward launch");
 }
 
 ec2moe_status ec2moe_lowrank_workspace_size(const ec2moe_codec_desc* desc, size_t* bytes) {

@@ -1,0 +1,41 @@
+// Interface of the 8-bit (e4m3) quantisation and products (fp8_quant.hip, fp8_gemm.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "gemm.h"
+#include "host_common.h"
+
+namespace ec2moe {
+
+constexpr int kFp8Block = 128;  // values that share a scale
+
+// x [n_mats][rows][cols] -> q, scale per block_rows (1 or 128) x 128 block
+hipError_t launch_fp8_quantize(DType dt, const void* x, int n_mats, int rows, int cols, int block_rows, void* q,
+                               float* scale, hipStream_t s);
+
+// out[p][n] = sum_k a[row(p)][k] w_e[n][k] for every row p of group e on the scaled values, row(p) =
+// row_index ? row_index[p] : p. SwiGLU: weight rows 0..N-1 are the gate branch and N..2N-1 the up
+// branch (N a multiple of 128), out = silu(gate) * up; ReLU: max(sum, 0).
+struct Fp8GemmArgs {
+    const uint8_t* a;         // [src_rows][K]
+    const float* a_scale;     // [src_rows][K / 128]
+    const int32_t* row_index; // gather map or null
+    const int32_t* seg;       // [groups+1] device segment offsets, or null (dense: one group)
+    int n_groups;
+    int64_t rows;             // total rows (upper bound for grouped; exact for dense)
+    int64_t src_rows;         // rows of a
+    const uint8_t* b;         // [groups][b_rows][K]
+    const float* b_scale;     // [groups][ceil(b_rows / 128)][K / 128]
+    int b_rows;
+    int K, N;
+    void* out;                // [rows][N] of out_type
+    const char* name;         // kernel name for the timing record
+};
+// Largest number of tiles of a launch (see fp8_gemm.hip): larger products are refused.
+bool fp8_gemm_fits(int64_t rows, int n_groups, int64_t n);
+hipError_t launch_fp8_gemm(Epilogue epi, DType out_type, const Fp8GemmArgs& a, hipStream_t s);
+
+}  // namespace ec2moe

@@ -1,0 +1,184 @@
+// Quantisation to 8-bit floating point (e4m3) with a float32 scale for each block of 128 columns of
+// a row, or of 128 x 128 values of a weight matrix, for gfx950.
+//
+//   amax = max(max |x|, 2^-100), scale = amax / 448, q = e4m3(448 x / amax)
+//
+// The quotient decides which 8-bit value is nearest, and bfloat16 inputs fall exactly half way
+// between two of them about once in a thousand values, so it is rounded as a true division is: with
+// r = 1 / amax and t = 448 x r, the step t + r (448 x - t amax), whose bracket is exact in a fused
+// multiply-add, lands on every quotient that has a short binary form. 4 instructions a value in place
+// of the 10 of the compiler's division.
+//
+// Memory-bound: one pass, every block's values stay in registers between its maximum and its
+// rounding. A NaN or an infinity shows in the maximum of the bit patterns without signs, which
+// orders like the magnitudes with infinity and NaN above them.
+#include "device_common.h"
+#include "fp8.h"
+
+namespace ec2moe {
+namespace {
+
+constexpr float kFp8Max = 448.f;
+constexpr uint32_t kAmaxMin = 0x0d800000u;  // 2^-100
+
+struct BlockScale {
+    float scale, amax, rcp, mul;  // mul: 448, or a power of two less for blocks where 448 x overflows
+    bool finite;
+};
+
+__device__ __forceinline__ BlockScale block_scale(uint32_t amax_bits) {
+    BlockScale b;
+    b.finite = amax_bits < 0x7f800000u;
+    float amax = __uint_as_float(max(amax_bits, kAmaxMin));
+    b.scale = b.finite ? amax / kFp8Max : __uint_as_float(0x7fc00000u);
+    const bool big = amax_bits >= 0x71800000u;  // 2^100
+    b.amax = big ? amax * 0x1p-32f : amax;
+    b.mul = big ? kFp8Max * 0x1p-32f : kFp8Max;
+    b.rcp = 1.0f / b.amax;
+    return b;
+}
+
+__device__ __forceinline__ float quotient(float x, const BlockScale& b) {
+    const float n = x * b.mul;
+    const float t = n * b.rcp;
+    return fmaf(b.rcp, fmaf(-t, b.amax, n), t);
+}
+
+// four values to four bytes
+__device__ __forceinline__ uint32_t quantize4(const float* x, const BlockScale& b) {
+    int w = 0;
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(x[0], b), quotient(x[1], b), w, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(x[2], b), quotient(x[3], b), w, true);
+    return b.finite ? static_cast<uint32_t>(w) : 0x7f7f7f7fu;
+}
+
+// 8 consecutive values as loaded: one or two 16-byte chunks
+template <typename T>
+struct Eight {
+    static constexpr int kChunks = 8 / Elem<T>::kPerChunk;
+    uint4 c[kChunks];
+    __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) c[i] = ldg16(p + i * Elem<T>::kPerChunk);
+    }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) c[i] = make_uint4(0, 0, 0, 0);
+    }
+    __device__ __forceinline__ void values(float (&v)[8]) const {
+        const T* e = reinterpret_cast<const T*>(c);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = Elem<T>::to_f32(e[i]);
+    }
+};
+
+__device__ __forceinline__ uint32_t magnitude_max(const float (&v)[8]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+    return m;
+}
+
+// A scale per row and 128 columns: rows are whole blocks, so the blocks are consecutive runs of 128
+// values whatever the matrix. 16 lanes take a block, a wave U times four of them.
+template <typename T, int U>
+__global__ __launch_bounds__(256) void quantize_rows_kernel(const T* __restrict__ x, int64_t n_blocks,
+                                                            uint8_t* __restrict__ q, float* __restrict__ scale) {
+    const int lane = threadIdx.x & 63;
+    const int64_t first = (static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6)) * (4 * U) + (lane >> 4);
+    Eight<T> in[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t b = first + 4 * u;
+        if (b < n_blocks) in[u].load(x + b * kFp8Block + (lane & 15) * 8);
+        else in[u].clear();
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t b = first + 4 * u;
+        float v[8];
+        in[u].values(v);
+        uint32_t m = magnitude_max(v);
+#pragma unroll
+        for (int off = 1; off < 16; off <<= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), off)));
+        const BlockScale bs = block_scale(m);
+        if (b >= n_blocks) continue;
+        *reinterpret_cast<uint2*>(q + b * kFp8Block + (lane & 15) * 8) = make_uint2(quantize4(v, bs), quantize4(v + 4, bs));
+        if ((lane & 15) == 0) scale[b] = bs.scale;
+    }
+}
+
+// A scale per 128 x 128 block: a workgroup per block, 16 lanes a row, 16 rows a pass.
+template <typename T>
+__global__ __launch_bounds__(256) void quantize_blocks_kernel(const T* __restrict__ x, int rows, int cols, int col_blocks,
+                                                              int row_blocks, uint8_t* __restrict__ q,
+                                                              float* __restrict__ scale) {
+    __shared__ uint32_t s_max[4];
+    const int64_t blk = blockIdx.x;  // (matrix, row block, column block)
+    const int cb = static_cast<int>(blk % col_blocks);
+    const int64_t mr = blk / col_blocks;
+    const int rb = static_cast<int>(mr % row_blocks);
+    const int64_t mat = mr / row_blocks;
+    const int tid = threadIdx.x;
+    const int r0 = rb * kFp8Block + tid / 16;
+    const int64_t base = (mat * rows + r0) * cols + cb * kFp8Block + (tid & 15) * 8;
+    Eight<T> in[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (r0 + 16 * i < rows) in[i].load(x + base + static_cast<int64_t>(16 * i) * cols);
+        else in[i].clear();
+    }
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float v[8];
+        in[i].values(v);
+        m = max(m, magnitude_max(v));
+    }
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), off)));
+    if ((tid & 63) == 0) s_max[tid >> 6] = m;
+    __syncthreads();
+    m = max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3]));
+    const BlockScale bs = block_scale(m);
+    if (tid == 0) scale[blk] = bs.scale;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (r0 + 16 * i >= rows) break;
+        float v[8];
+        in[i].values(v);
+        *reinterpret_cast<uint2*>(q + base + static_cast<int64_t>(16 * i) * cols) =
+            make_uint2(quantize4(v, bs), quantize4(v + 4, bs));
+    }
+}
+
+template <typename T>
+hipError_t run(const T* x, int n_mats, int rows, int cols, int block_rows, uint8_t* q, float* scale, hipStream_t s) {
+    const int cb = cols / kFp8Block;
+    if (block_rows == 1) {
+        const int64_t n = static_cast<int64_t>(n_mats) * rows * cb;
+        constexpr int U = 4;
+        const int64_t grid = (n + 16 * U - 1) / (16 * U);
+        hipLaunchKernelGGL((quantize_rows_kernel<T, U>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, s, x, n, q, scale);
+    } else {
+        const int rb = (rows + kFp8Block - 1) / kFp8Block;
+        const int64_t grid = static_cast<int64_t>(n_mats) * rb * cb;
+        hipLaunchKernelGGL((quantize_blocks_kernel<T>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, s, x, rows, cols, cb,
+                           rb, q, scale);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_fp8_quantize(DType dt, const void* x, int n_mats, int rows, int cols, int block_rows, void* q,
+                               float* scale, hipStream_t s) {
+    if (n_mats == 0 || rows == 0) return hipSuccess;
+    const char* blocks = "fp8_quantize_blocks";  // weights: outside the layer step
+    ProfileScope prof(block_rows != 1 ? blocks : "fp8_quantize_rows", s);
+    uint8_t* q8 = static_cast<uint8_t*>(q);
+    if (dt == DType::BF16) return run(static_cast<const bf16_t*>(x), n_mats, rows, cols, block_rows, q8, scale, s);
+    return run(static_cast<const float*>(x), n_mats, rows, cols, block_rows, q8, scale, s);
+}
+
+}  // namespace ec2moe

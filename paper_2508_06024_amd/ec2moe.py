@@ -50,6 +50,15 @@ class GateOpts(ctypes.Structure):
                 ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
 
 
+class Fp8MatmulDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("n_groups", ctypes.c_int32), ("n", ctypes.c_int32), ("k", ctypes.c_int32),
+                ("out_dtype", ctypes.c_int)]
+
+
+class GateGrads(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("d_topk_w", "d_probs", "d_balance", "token_valid")]
+
+
 class DeviceState(ctypes.Structure):
     _fields_ = [("cpu", ctypes.c_double), ("mem", ctypes.c_double), ("power", ctypes.c_double),
                 ("bandwidth", ctypes.c_double)]
@@ -95,6 +104,16 @@ _SIGS = {
     "ec2moe_lowrank_decode": [ctypes.POINTER(CodecDesc), _P, _P, _P, _P, _P, ctypes.c_size_t, _P],
     "ec2moe_lowrank_fit_workspace_size": [ctypes.POINTER(CodecDesc), ctypes.POINTER(ctypes.c_size_t)],
     "ec2moe_lowrank_fit": [ctypes.POINTER(CodecDesc), _P, _P, _P, ctypes.c_int32, _P, _P, _P, _P, ctypes.c_size_t, _P],
+    "ec2moe_fp8_quantize": [_P, ctypes.c_int, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _P, _P, _P],
+    "ec2moe_fp8_matmul_workspace_size": [ctypes.POINTER(Fp8MatmulDesc), ctypes.POINTER(ctypes.c_size_t)],
+    "ec2moe_fp8_matmul": [ctypes.POINTER(Fp8MatmulDesc), _P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P],
+    "ec2moe_fp8_moe_workspace_size": [ctypes.POINTER(MoeDesc), ctypes.POINTER(ctypes.c_size_t)],
+    "ec2moe_fp8_moe_forward": [ctypes.POINTER(MoeDesc), _P, _P, _P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P],
+    "ec2moe_balance_loss_workspace_size": [ctypes.POINTER(MoeDesc), ctypes.POINTER(ctypes.c_size_t)],
+    "ec2moe_balance_loss": [ctypes.POINTER(MoeDesc), _P, _P, _P, ctypes.c_float, _P, _P, _P, _P, ctypes.c_size_t, _P],
+    "ec2moe_gate_backward_workspace_size": [ctypes.POINTER(MoeDesc), ctypes.POINTER(ctypes.c_size_t)],
+    "ec2moe_group_gate_backward": [ctypes.POINTER(MoeDesc), ctypes.POINTER(GateOpts), ctypes.POINTER(GateGrads),
+                                   _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P],
     "ec2moe_status_string": [ctypes.c_int],
     "ec2moe_last_error": [],
     "ec2moe_profile_enable": [ctypes.c_int32],
@@ -351,6 +370,214 @@ def moe_forward(x, topk_idx, topk_w, w_gate_up, w_down, ws=None, activation="swi
     y = torch.empty((T, d), dtype=dt, device=x.device)
     moe_forward_into(desc, x, topk_idx, topk_w, w_gate_up, w_down, y, ws)
     return y
+
+
+# ----------------------------------------------------------------------------- 8-bit experts
+
+FP8 = torch.float8_e4m3fn
+FP8_BLOCK = 128
+
+
+def _dev_here(t: torch.Tensor, name: str, dtype=None, shape=None):
+    """_dev for a tensor that also has to lie on the current device, whose stream takes the call."""
+    _dev(t, name, dtype, shape)
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return t
+
+
+def _blocks(n: int) -> int:
+    return -(-n // FP8_BLOCK)
+
+
+def fp8_quantize_into(x, q, scale, block_rows=1):
+    """Raw call: x [n_mats][rows][cols] (or [rows][cols]) into q of the same shape and scale."""
+    rows, cols = x.shape[-2:]
+    _check(_lib.ec2moe_fp8_quantize(_ptr(x), dtype_code(x.dtype), x.shape[0] if x.dim() == 3 else 1, rows, cols, block_rows,
+                                    _ptr(q), _ptr(scale), _stream()))
+
+
+def fp8_quantize(x, block_rows=1):
+    """x [rows][cols] or [n_mats][rows][cols] as e4m3 values and float32 scales: one per row and 128
+    columns (block_rows 1, activations) or per 128 x 128 block (block_rows 128, weights)."""
+    if x.dim() not in (2, 3):
+        raise ValueError(f"x has {x.dim()} dimensions, expected 2 or 3")
+    if block_rows not in (1, FP8_BLOCK):
+        raise ValueError(f"block_rows must be 1 or {FP8_BLOCK}, got {block_rows}")
+    dtype_code(x.dtype)
+    _dev_here(x, "x")
+    rows, cols = x.shape[-2:]
+    q = torch.empty(x.shape, dtype=FP8, device=x.device)
+    scale = torch.empty((*x.shape[:-2], -(-rows // block_rows), cols // FP8_BLOCK), dtype=torch.float32, device=x.device)
+    fp8_quantize_into(x, q, scale, block_rows)
+    return q, scale
+
+
+def fp8_matmul_desc(rows, n_groups, n, k, out_dtype) -> Fp8MatmulDesc:
+    return Fp8MatmulDesc(rows, n_groups, n, k, out_dtype if isinstance(out_dtype, int) else dtype_code(out_dtype))
+
+
+def fp8_matmul_workspace_size(desc: Fp8MatmulDesc) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib.ec2moe_fp8_matmul_workspace_size(ctypes.byref(desc), ctypes.byref(n)))
+    return n.value
+
+
+def fp8_matmul_into(desc: Fp8MatmulDesc, a, a_scale, seg_offsets, b, b_scale, out, ws):
+    """Raw call with caller-owned output and workspace (no allocation)."""
+    _check(_lib.ec2moe_fp8_matmul(ctypes.byref(desc), _ptr(a), _ptr(a_scale), _ptr(seg_offsets), _ptr(b), _ptr(b_scale),
+                                  _ptr(out), _ptr(ws), ws.numel(), _stream()))
+
+
+def fp8_matmul(a, a_scale, b, b_scale, seg_offsets=None, out_dtype=torch.bfloat16, out=None, ws=None):
+    """a [rows][k] by the weights of each row's group: b [n][k] (every row), or b [n_groups][n][k] with
+    seg_offsets [n_groups + 1]. Rows behind the last segment keep what out holds (zeros when it is
+    made here)."""
+    bs = b if b.dim() == 3 else b.unsqueeze(0)
+    ss = b_scale if b_scale.dim() == 3 else b_scale.unsqueeze(0)
+    G, n, k = bs.shape
+    rows = a.shape[0]
+    _dev_here(a, "a", FP8, (rows, k))
+    _dev_here(a_scale, "a_scale", torch.float32, (rows, k // FP8_BLOCK))
+    _dev_here(bs, "b", FP8)
+    _dev_here(ss, "b_scale", torch.float32, (G, _blocks(n), k // FP8_BLOCK))
+    if seg_offsets is not None:
+        _dev_here(seg_offsets, "seg_offsets", torch.int32, (G + 1,))
+    if out is None:
+        new = torch.empty if seg_offsets is None else torch.zeros
+        out = new((rows, n), dtype=out_dtype, device=a.device)
+    _dev_here(out, "out", None, (rows, n))
+    desc = fp8_matmul_desc(rows, G, n, k, out.dtype)
+    ws = ws if ws is not None else workspace(fp8_matmul_workspace_size(desc), a.device)
+    fp8_matmul_into(desc, a, a_scale, seg_offsets, bs, ss, out, ws)
+    return out
+
+
+def fp8_moe_workspace_size(desc: MoeDesc) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib.ec2moe_fp8_moe_workspace_size(ctypes.byref(desc), ctypes.byref(n)))
+    return n.value
+
+
+def fp8_moe_forward_into(desc: MoeDesc, x, topk_idx, topk_w, w_gate_up, w_gate_up_scale, w_down, w_down_scale, y, ws):
+    """Raw call with caller-owned output and workspace (no allocation)."""
+    _check(_lib.ec2moe_fp8_moe_forward(ctypes.byref(desc), _ptr(x), _ptr(topk_idx), _ptr(topk_w), _ptr(w_gate_up),
+                                       _ptr(w_gate_up_scale), _ptr(w_down), _ptr(w_down_scale), _ptr(y), _ptr(ws),
+                                       ws.numel(), _stream()))
+
+
+def _check_fp8_experts(w_gate_up, w_gate_up_scale, w_down, w_down_scale, d, activation):
+    M, _, H = w_down.shape
+    rows = w_in_rows(H, activation)
+    _dev_here(w_gate_up, "w_gate_up", FP8, (M, rows, d))
+    _dev_here(w_gate_up_scale, "w_gate_up_scale", torch.float32, (M, _blocks(rows), d // FP8_BLOCK))
+    _dev_here(w_down, "w_down", FP8, (M, d, H))
+    _dev_here(w_down_scale, "w_down_scale", torch.float32, (M, _blocks(d), H // FP8_BLOCK))
+    return M, H
+
+
+def fp8_moe_forward(x, topk_idx, topk_w, w_gate_up, w_gate_up_scale, w_down, w_down_scale, ws=None,
+                    activation="swiglu"):
+    """moe_forward with 8-bit expert weights and their 128 x 128 block scales (fp8_quantize with
+    block_rows 128)."""
+    T, d = x.shape
+    k = topk_idx.shape[1]
+    dt = x.dtype
+    _dev_here(x, "x")
+    _dev_here(topk_idx, "topk_idx", torch.int32, (T, k))
+    _dev_here(topk_w, "topk_w", torch.float32, (T, k))
+    M, H = _check_fp8_experts(w_gate_up, w_gate_up_scale, w_down, w_down_scale, d, activation)
+    desc = moe_desc(T, M, 1, d, H, k, dt, activation=activation)
+    ws = ws if ws is not None else workspace(fp8_moe_workspace_size(desc), x.device)
+    y = torch.empty((T, d), dtype=dt, device=x.device)
+    fp8_moe_forward_into(desc, x, topk_idx, topk_w, w_gate_up, w_gate_up_scale, w_down, w_down_scale, y, ws)
+    return y
+
+
+# ----------------------------------------------------------------------------- training the router
+
+def _valid_bytes(token_valid, T):
+    """token_valid [T] bool or uint8 as the library's bytes."""
+    if token_valid is None:
+        return None
+    if token_valid.dtype not in (torch.bool, torch.uint8):
+        raise TypeError(f"token_valid has dtype {token_valid.dtype}, expected torch.bool or torch.uint8")
+    return _dev_here(token_valid, "token_valid", None, (T,))
+
+
+def balance_loss_workspace_size(desc: MoeDesc) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib.ec2moe_balance_loss_workspace_size(ctypes.byref(desc), ctypes.byref(n)))
+    return n.value
+
+
+def balance_loss_into(desc: MoeDesc, probs, topk_idx, coef, loss, counts, d_probs, ws, token_valid=None):
+    """Raw call with caller-owned outputs (counts and d_probs may be None) and workspace."""
+    _check(_lib.ec2moe_balance_loss(ctypes.byref(desc), _ptr(probs), _ptr(topk_idx), _ptr(token_valid), float(coef),
+                                    _ptr(counts), _ptr(loss), _ptr(d_probs), _ptr(ws), ws.numel(), _stream()))
+
+
+def balance_loss(probs, topk_idx, coef=1.0, token_valid=None, ws=None):
+    """(loss [1], counts [M] int32, d_probs [M]) of the routing probs [T][M], topk_idx [T][k]: coef * M *
+    sum of f_i P_i, and its gradient with respect to every valid token's probs (the d_balance of
+    group_gate_backward)."""
+    T, M = probs.shape
+    k = topk_idx.shape[1]
+    _dev_here(probs, "probs", torch.float32)
+    _dev_here(topk_idx, "topk_idx", torch.int32, (T, k))
+    desc = moe_desc(T, M, 1, FP8_BLOCK, FP8_BLOCK, k, BF16)
+    ws = ws if ws is not None else workspace(balance_loss_workspace_size(desc), probs.device)
+    loss = torch.empty((1,), dtype=torch.float32, device=probs.device)
+    counts = torch.empty((M,), dtype=torch.int32, device=probs.device)
+    d_probs = torch.empty((M,), dtype=torch.float32, device=probs.device)
+    balance_loss_into(desc, probs, topk_idx, coef, loss, counts, d_probs, ws, _valid_bytes(token_valid, T))
+    return loss, counts, d_probs
+
+
+def gate_backward_workspace_size(desc: MoeDesc) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib.ec2moe_gate_backward_workspace_size(ctypes.byref(desc), ctypes.byref(n)))
+    return n.value
+
+
+def group_gate_backward_into(desc: MoeDesc, opts: Optional[GateOpts], x, w_global, w_local, probs, topk_idx, ws,
+                             d_topk_w=None, d_probs=None, d_balance=None, token_valid=None, d_x=None, d_w_global=None,
+                             d_b_global=None, d_w_local=None, d_b_local=None):
+    """Raw call with caller-owned outputs (None: not computed) and workspace."""
+    addr = lambda t: None if t is None else t.data_ptr()
+    grads = GateGrads(addr(d_topk_w), addr(d_probs), addr(d_balance), addr(token_valid))
+    _check(_lib.ec2moe_group_gate_backward(ctypes.byref(desc), ctypes.byref(opts) if opts is not None else None,
+                                           ctypes.byref(grads), _ptr(x), _ptr(w_global), _ptr(w_local), _ptr(probs),
+                                           _ptr(topk_idx), _ptr(d_x), _ptr(d_w_global), _ptr(d_b_global), _ptr(d_w_local),
+                                           _ptr(d_b_local), _ptr(ws), ws.numel(), _stream()))
+
+
+def group_gate_backward(x, w_global, w_local, probs, topk_idx, d_topk_w=None, d_probs=None, d_balance=None,
+                        token_valid=None, renormalize=True, group_sizes=None, with_dx=True, ws=None):
+    """Gradients (d_x, d_w_global, d_b_global, d_w_local, d_b_local) of the gate's inputs from those of
+    its outputs: d_topk_w [T][k], d_probs [T][M], and d_balance [M], which every valid token shares.
+    The gate must have kept every group (top_groups 0). d_x (None without with_dx) has x's type, the
+    others are float32."""
+    T, d = x.shape
+    M, K = w_local.shape[0], w_global.shape[0]
+    k = topk_idx.shape[1]
+    dt = x.dtype
+    _dev_here(x, "x")
+    _dev_here(w_global, "w_global", dt, (K, d))
+    _dev_here(w_local, "w_local", dt, (M, d))
+    _dev_here(probs, "probs", torch.float32, (T, M))
+    _dev_here(topk_idx, "topk_idx", torch.int32, (T, k))
+    for t, name, shape in ((d_topk_w, "d_topk_w", (T, k)), (d_probs, "d_probs", (T, M)), (d_balance, "d_balance", (M,))):
+        if t is not None:
+            _dev_here(t, name, torch.float32, shape)
+    desc = moe_desc(T, M, K, d, FP8_BLOCK, k, dt, renormalize)
+    ws = ws if ws is not None else workspace(gate_backward_workspace_size(desc), x.device)
+    new = lambda *shape: torch.empty(shape, dtype=torch.float32, device=x.device)
+    d_x = torch.empty_like(x) if with_dx else None
+    d_wg, d_bg, d_wl, d_bl = new(K, d), new(K), new(M, d), new(M)
+    group_gate_backward_into(desc, gate_opts(0, group_sizes), x, w_global, w_local, probs, topk_idx, ws, d_topk_w, d_probs,
+                             d_balance, _valid_bytes(token_valid, T), d_x, d_wg, d_bg, d_wl, d_bl)
+    return d_x, d_wg, d_bg, d_wl, d_bl
 
 
 # ----------------------------------------------------------------------------- codec

@@ -17,6 +17,10 @@ the current one, so that it overlaps the codec; the expert GEMMs and the combine
 the current stream. The kernels and their inputs are those of the one-stream order, so
 the results are bit-identical. It is off by default: the cross-stream join costs about as
 much as the overlap saves on the workloads measured, and more on the small ones.
+
+Expert weights in 8-bit floating point (w_gate_up and w_down of torch.float8_e4m3fn, with
+expert_scales = (w_gate_up_scale, w_down_scale), as from ec2moe.fp8_quantize with block_rows 128)
+run through fp8_moe_forward in place of moe_forward; everything before the experts is the same.
 """
 from __future__ import annotations
 
@@ -28,7 +32,7 @@ from . import ec2moe as E
 class Ec2moeLayer:
     def __init__(self, x, mask_words, w_global, b_global, w_local, b_local, w_gate_up, w_down, u, v,
                  u_hat=None, v_hat=None, n_groups=1, top_k=1, renormalize=True, activation="swiglu",
-                 codec_slices=1, top_groups=0, group_sizes=None, overlap=False):
+                 codec_slices=1, top_groups=0, group_sizes=None, overlap=False, expert_scales=None):
         T, d = x.shape
         M, _, H = w_down.shape
         dt = x.dtype
@@ -36,6 +40,9 @@ class Ec2moeLayer:
         self.x, self.mask = x, list(mask_words)
         self.w_global, self.b_global, self.w_local, self.b_local = w_global, b_global, w_local, b_local
         self.w_gate_up, self.w_down = w_gate_up, w_down
+        self.expert_scales = expert_scales
+        if (expert_scales is not None) != (w_gate_up.dtype == E.FP8):
+            raise ValueError("expert_scales go with 8-bit expert weights")
         self.u, self.v = u, v
         self.u_hat = u if u_hat is None else u_hat
         self.v_hat = v if v_hat is None else v_hat
@@ -54,7 +61,13 @@ class Ec2moeLayer:
         self.z = torch.empty((codec_slices, u.shape[1], v.shape[1]), dtype=torch.float32, device=dev)
         self.x_hat = torch.empty((T, d), dtype=dt, device=dev)
         self.y = torch.empty((T, d), dtype=dt, device=dev)
-        self.moe_ws = E.workspace(E.moe_workspace_size(self.moe_desc), dev)
+        if expert_scales is None:
+            self.moe_ws = E.workspace(E.moe_workspace_size(self.moe_desc), dev)
+        else:
+            if overlap:
+                raise ValueError("overlap needs the layer dtype's experts")
+            E._check_fp8_experts(w_gate_up, expert_scales[0], w_down, expert_scales[1], d, activation)
+            self.moe_ws = E.workspace(E.fp8_moe_workspace_size(self.moe_desc), dev)
         self.overlap = overlap
         if overlap:
             A = T * top_k
@@ -88,6 +101,12 @@ class Ec2moeLayer:
         E.lowrank_decode_into(self.codec_desc, self.z, self.u_hat, self.v_hat, self.x_hat, self.codec_ws)
 
     def step(self):
+        if self.expert_scales is not None:
+            self._gate()
+            self._codec()
+            E.fp8_moe_forward_into(self.moe_desc, self.x_hat, self.topk_idx, self.topk_w, self.w_gate_up,
+                                   self.expert_scales[0], self.w_down, self.expert_scales[1], self.y, self.moe_ws)
+            return self.y
         if not self.overlap:
             self._gate()
             self._codec()
