@@ -568,6 +568,7 @@ struct Fp8MoeWs {
 
 Fp8MoeWs fp8_moe_ws(const ec2moe_moe_desc* d) {
     const int64_t T = d->n_tokens, A = T * d->top_k, kb = d->d_model / kFp8Block, hb = d->ffn_hidden / kFp8Block;
+    const Epilogue epi = d->flags & EC2MOE_EXPERT_RELU ? Epilogue::ReLU : Epilogue::SwiGLU;
     Fp8MoeWs w{};
     size_t o = 0;
     w.counts = o; o += up(static_cast<size_t>(std::max(1, perm_chunks(A))) * d->n_experts * 4);
@@ -576,7 +577,7 @@ Fp8MoeWs fp8_moe_ws(const ec2moe_moe_desc* d) {
     w.inv_perm = o; o += up(static_cast<size_t>(A) * 4);
     w.xq = o; o += up(static_cast<size_t>(T) * d->d_model);
     w.xs = o; o += up(static_cast<size_t>(T) * kb * 4);
-    w.act = o; o += up(static_cast<size_t>(A) * d->ffn_hidden * 4);
+    w.act = o; o += up(fp8_hidden_scratch_bytes(epi, A, d->n_experts, d->d_model, d->ffn_hidden));
     w.act_q = o; o += up(static_cast<size_t>(A) * d->ffn_hidden);
     w.act_s = o; o += up(static_cast<size_t>(A) * hb * 4);
     w.y_perm = o; o += up(static_cast<size_t>(A) * d->d_model * elem_bytes(static_cast<DType>(d->dtype)));
@@ -607,8 +608,7 @@ ec2moe_status ec2moe_fp8_matmul(const ec2moe_fp8_matmul_desc* desc, const void* 
     g.a = static_cast<const uint8_t*>(a); g.a_scale = a_scale; g.seg = seg_offsets; g.n_groups = desc->n_groups;
     g.rows = desc->rows; g.src_rows = desc->rows; g.b = static_cast<const uint8_t*>(b); g.b_scale = b_scale;
     g.b_rows = desc->n; g.K = desc->k; g.N = desc->n; g.out = out; g.name = kFp8MatmulName;
-    return hip_status(launch_fp8_gemm(Epilogue::Store, static_cast<DType>(desc->out_dtype), g, stream),
-                      "fp8_matmul launch");
+    return hip_status(launch_fp8_gemm(static_cast<DType>(desc->out_dtype), g, stream), "fp8_matmul launch");
 }
 
 ec2moe_status ec2moe_fp8_moe_workspace_size(const ec2moe_moe_desc* desc, size_t* bytes) {
@@ -646,19 +646,16 @@ ec2moe_status ec2moe_fp8_moe_forward(const ec2moe_moe_desc* desc, const void* x,
         Fp8GemmArgs g{};
         g.a = at<uint8_t>(ws, w.xq); g.a_scale = at<float>(ws, w.xs); g.row_index = perm_src; g.seg = seg;
         g.n_groups = M; g.rows = A; g.src_rows = T; g.b = static_cast<const uint8_t*>(w_gate_up);
-        g.b_scale = w_gate_up_scale; g.b_rows = relu ? H : 2 * H; g.K = d; g.N = H; g.out = at<void>(ws, w.act);
-        g.name = relu ? "fp8_expert_in_relu" : "fp8_expert_gate_up";
-        e = launch_fp8_gemm(relu ? Epilogue::ReLU : Epilogue::SwiGLU, DType::F32, g, stream);
+        g.b_scale = w_gate_up_scale; g.b_rows = relu ? H : 2 * H; g.K = d; g.N = H; g.out = at<void>(ws, w.act_q);
+        g.out_scale = at<float>(ws, w.act_s); g.name = relu ? "fp8_expert_in_relu" : "fp8_expert_gate_up";
+        e = launch_fp8_hidden(relu ? Epilogue::ReLU : Epilogue::SwiGLU, g, at<float>(ws, w.act), stream);
     }
-    if (e == hipSuccess)
-        e = launch_fp8_quantize(DType::F32, at<void>(ws, w.act), 1, static_cast<int>(A), H, 1, at<void>(ws, w.act_q),
-                                at<float>(ws, w.act_s), stream);
     if (e == hipSuccess) {
         Fp8GemmArgs g{};
         g.a = at<uint8_t>(ws, w.act_q); g.a_scale = at<float>(ws, w.act_s); g.seg = seg; g.n_groups = M; g.rows = A;
         g.src_rows = A; g.b = static_cast<const uint8_t*>(w_down); g.b_scale = w_down_scale; g.b_rows = d; g.K = H;
         g.N = d; g.out = at<void>(ws, w.y_perm); g.name = "fp8_expert_down";
-        e = launch_fp8_gemm(Epilogue::Store, dt, g, stream);
+        e = launch_fp8_gemm(dt, g, stream);
     }
     if (e == hipSuccess)
         e = launch_combine(dt, at<void>(ws, w.y_perm), inv_perm, topk_w, T, desc->top_k, d, y, stream);

@@ -17,8 +17,7 @@ hipError_t launch_fp8_quantize(DType dt, const void* x, int n_mats, int rows, in
                                float* scale, hipStream_t s);
 
 // out[p][n] = sum_k a[row(p)][k] w_e[n][k] for every row p of group e on the scaled values, row(p) =
-// row_index ? row_index[p] : p. SwiGLU: weight rows 0..N-1 are the gate branch and N..2N-1 the up
-// branch (N a multiple of 128), out = silu(gate) * up; ReLU: max(sum, 0).
+// row_index ? row_index[p] : p.
 struct Fp8GemmArgs {
     const uint8_t* a;         // [src_rows][K]
     const float* a_scale;     // [src_rows][K / 128]
@@ -31,11 +30,20 @@ struct Fp8GemmArgs {
     const float* b_scale;     // [groups][ceil(b_rows / 128)][K / 128]
     int b_rows;
     int K, N;
-    void* out;                // [rows][N] of out_type
+    void* out;                // [rows][N]
+    float* out_scale;         // [rows][N / 128] (hidden rows)
     const char* name;         // kernel name for the timing record
 };
 // Largest number of tiles of a launch (see fp8_gemm.hip): larger products are refused.
 bool fp8_gemm_fits(int64_t rows, int n_groups, int64_t n);
-hipError_t launch_fp8_gemm(Epilogue epi, DType out_type, const Fp8GemmArgs& a, hipStream_t s);
+// out of out_type. Float32 outputs and few rows a group: exact products (through bfloat16); else those of
+// the 8-bit matrix core.
+hipError_t launch_fp8_gemm(DType out_type, const Fp8GemmArgs& a, hipStream_t s);
+
+// Hidden rows of the experts: SwiGLU (weight rows 0..N-1 are the gate branch and N..2N-1 the up branch), silu(gate)
+// * up, or ReLU, max(sum, 0); N and K multiples of 128. Quantised by rows from their float32 values to out and
+// out_scale, by way of scratch (fp8_hidden_scratch_bytes) where the product's tiles do not hold whole blocks.
+size_t fp8_hidden_scratch_bytes(Epilogue epi, int64_t rows, int n_groups, int K, int N);
+hipError_t launch_fp8_hidden(Epilogue epi, const Fp8GemmArgs& a, float* scratch, hipStream_t s);
 
 }  // namespace ec2moe

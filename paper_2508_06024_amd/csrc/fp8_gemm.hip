@@ -3,28 +3,29 @@
 //
 //   out[p][n] = sum_kb sa[row(p)][kb] sb_e[n / 128][kb] sum_{k in kb} a[row(p)][k] w_e[n][k]
 //
-// for every row p of group e. v_mfma_f32_16x16x128_f8f6f4 contracts one block of 128 in one
-// instruction, so its result is scaled by sa sb and added to the float32 accumulators by four
-// fused multiply-adds a lane. Weight rows feed the A operand and token rows the B operand: a lane ends
-// with 4 consecutive output columns of one token row. Both operands give lane group g of a wave the
-// bytes 16 g .. + 15 and 64 + 16 g .. + 15 of the block; any assignment that both share covers it.
+// for every row p of group e. A block of 128 is contracted into fresh accumulators, which four fused
+// multiply-adds a lane scale by sa sb and add to the float32 sums. Weight rows feed the A operand and
+// token rows the B operand: a lane ends with 4 consecutive output columns of one token row.
+//
+// Three kernels:
+//   * fp8_skinny_kernel (few rows a group): a stream of the weights, straight from memory to registers;
+//   * fp8_ring_kernel (64-row tiles): operands through a ring of LDS slabs;
+//   * fp8_pp_kernel (256 x 256 tiles): two groups of waves that alternate between products and memory.
+// The first two multiply exactly, through bfloat16, for float32 outputs (and the first always: a stream of
+// weights leaves the matrix cores idle); the others use the 8-bit matrix core, at twice the rate.
 #include "device_common.h"
-#include "fp8.h"
+#include "fp8_device.h"
 #include "gemm_tiles.h"
 
 namespace ec2moe {
 namespace {
 
-typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(4))) float cfloat;  // constant memory
 
-__device__ __forceinline__ i32x8 frag(uint4 lo, uint4 hi) {
-    return i32x8{static_cast<int>(lo.x), static_cast<int>(lo.y), static_cast<int>(lo.z), static_cast<int>(lo.w),
-                 static_cast<int>(hi.x), static_cast<int>(hi.y), static_cast<int>(hi.z), static_cast<int>(hi.w)};
-}
+__device__ __forceinline__ float relu(float v) { return v < 0.f ? 0.f : v; }  // NaN stays
 
-__device__ __forceinline__ f32x4 mfma8(i32x8 a, i32x8 b) {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
-}
+__device__ __forceinline__ int scale_rows(const Fp8GemmArgs& p) { return (p.b_rows + kFp8Block - 1) / kFp8Block; }
 
 template <typename TO>
 __device__ __forceinline__ void store_run(TO* dst, f32x4 v, int left, bool whole) {
@@ -44,6 +45,8 @@ __device__ __forceinline__ void store_run(TO* dst, f32x4 v, int left, bool whole
         if (i < left) dst[i] = Elem<TO>::from_f32(v[i]);
 }
 
+// ------------------------------------------------------------------ few rows
+//
 // A tile of 16 MT token rows and 16 NT weight rows (SwiGLU: NT gate and NT up blocks) by WAVES waves that
 // take every WAVES-th block of K, fragments straight from memory; their sums meet in LDS and are added
 // in wave order.
@@ -64,7 +67,7 @@ __global__ __launch_bounds__(64 * WAVES) void fp8_skinny_kernel(Fp8GemmArgs p) {
     const uint8_t* wrow[NB];
     const float* wscale[NB];
     const uint8_t* wg = p.b + static_cast<int64_t>(ti.group) * p.b_rows * p.K;
-    const float* sg = p.b_scale + static_cast<int64_t>(ti.group) * ((p.b_rows + kFp8Block - 1) / kFp8Block) * nkb;
+    const float* sg = p.b_scale + static_cast<int64_t>(ti.group) * scale_rows(p) * nkb;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
         const int r0 = SWIGLU && nb >= NT ? p.N + n0 + (nb - NT) * 16 : n0 + nb * 16;
@@ -93,23 +96,28 @@ __global__ __launch_bounds__(64 * WAVES) void fp8_skinny_kernel(Fp8GemmArgs p) {
         float sw[NB], st[MT];
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-            fw[nb] = frag(ldg16(wrow[nb] + off), ldg16(wrow[nb] + off + 64));
+            fw[nb] = frag8(ldg16(wrow[nb] + off), ldg16(wrow[nb] + off + 64));
             sw[nb] = wscale[nb][kb];
         }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            ft[mt] = frag(ldg16(trow[mt] + off), ldg16(trow[mt] + off + 64));
+            ft[mt] = frag8(ldg16(trow[mt] + off), ldg16(trow[mt] + off + 64));
             st[mt] = tscale[mt][kb];
         }
+        Wide wt[MT];
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
+        for (int mt = 0; mt < MT; ++mt) wt[mt] = widen(ft[mt]);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const Wide ww = widen(fw[nb]);
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
-                const f32x4 part = mfma8(fw[nb], ft[mt]);
+                const f32x4 part = mfma_wide(ww, wt[mt]);
                 const float s = sw[nb] * st[mt];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[nb][mt][i] = fmaf(part[i], s, acc[nb][mt][i]);
             }
+        }
     }
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
@@ -132,7 +140,7 @@ __global__ __launch_bounds__(64 * WAVES) void fp8_skinny_kernel(Fp8GemmArgs p) {
             for (int i = 0; i < 4; ++i) v[i] = silu(v[i]) * u[i];
         } else if constexpr (EPI == Epilogue::ReLU) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];
+            for (int i = 0; i < 4; ++i) v[i] = relu(v[i]);
         }
         const int r = mt * 16 + l16, c = n0 + nb * 16 + 4 * lg;
         if (r < ti.valid && c < p.N)
@@ -140,27 +148,623 @@ __global__ __launch_bounds__(64 * WAVES) void fp8_skinny_kernel(Fp8GemmArgs p) {
     }
 }
 
+// Weight row (within the group's matrix) of tile row n: SwiGLU tiles hold TN/2 gate rows, then the matching up
+// rows; rows past the matrix repeat its last one (their columns are not stored).
+template <int TN, bool SWIGLU>
+__device__ __forceinline__ int weight_row(const Fp8GemmArgs& p, int nt, int n) {
+    if (SWIGLU) return n < TN / 2 ? nt * (TN / 2) + n : p.N + nt * (TN / 2) + (n - TN / 2);
+    return std::min(nt * TN + n, p.b_rows - 1);
+}
+
+// ------------------------------------------------------------------ 64-row tiles through a ring
+//
+// Tiles of TM x 128 over the whole K: slabs of one block of 128 (128-byte pieces of each row) go through
+// a ring of RING LDS stages filled by buffer_load ... lds, RING - 1 of them in flight behind counted waits
+// and one barrier per slab. Four waves of TM x 32. Chunk c of staged row R sits at c ^ ((R >> 1) & 7).
+// EXACT: products through bfloat16.
+template <typename TO, int TM, int RING, Epilogue EPI, bool EXACT>
+__global__ __launch_bounds__(256, 2) void fp8_ring_kernel(Fp8GemmArgs p) {
+    constexpr bool SWIGLU = EPI == Epilogue::SwiGLU;
+    constexpr int TN = 128;
+    constexpr int NLD = (TM + TN) / 32;  // load instructions (8 rows) per wave per slab
+    constexpr int MI = TM / 16, NI = 2;
+    constexpr int NOUT = SWIGLU ? TN / 2 : TN;
+    constexpr int STAGE = (TM + TN) * kFp8Block;
+    static_assert((TM + TN) % 32 == 0 && TM % 16 == 0, "whole load instructions");
+    static_assert(RING == 3 || RING == 4, "ring of 3 or 4 slabs");
+    __shared__ __attribute__((aligned(1024))) char lds0[STAGE];
+    __shared__ __attribute__((aligned(1024))) char lds1[STAGE];
+    __shared__ __attribute__((aligned(1024))) char lds2[STAGE];
+    __shared__ __attribute__((aligned(1024))) char lds3[RING > 3 ? STAGE : 16];
+
+    const int ntn = (p.N + NOUT - 1) / NOUT;
+    TileInfo ti;
+    if (!find_tile<TM>(p, ntn, ti)) return;
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    const int lane = tid & 63, wave = uniform(tid >> 6);
+    const int l16 = lane & 15, lg = lane >> 4;
+    const int K = p.K, nkb = K / kFp8Block;
+
+    auto swz = [](int R) { return (R >> 1) & 7; };
+    // contiguous token rows: the descriptor starts at the tile, so that offsets stay within 32 bits
+    const uint8_t* abase = p.row_index ? p.a : p.a + ti.row0 * K;
+    const i32x4 rtok = buffer_rsrc(abase, static_cast<uint32_t>(p.row_index ? p.src_rows * K : static_cast<int64_t>(ti.valid) * K));
+    const i32x4 rw = buffer_rsrc(p.b + static_cast<int64_t>(ti.group) * p.b_rows * K,
+                                 static_cast<uint32_t>(static_cast<int64_t>(p.b_rows) * K));
+    uint32_t voff[NLD];
+#pragma unroll
+    for (int j = 0; j < NLD; ++j) {
+        const int R = 8 * (NLD * wave + j) + lane / 8;
+        uint32_t src;
+        if (R < TM) {
+            const int r = std::min(R, ti.valid - 1);
+            src = p.row_index ? static_cast<uint32_t>(p.row_index[ti.row0 + r]) : static_cast<uint32_t>(r);
+        } else {
+            src = static_cast<uint32_t>(weight_row<TN, SWIGLU>(p, ti.nt, R - TM));
+        }
+        voff[j] = src * static_cast<uint32_t>(K) + static_cast<uint32_t>(((lane % 8) ^ swz(R)) * 16);
+    }
+    auto issue = [&](int st, char* slot) {
+#pragma unroll
+        for (int j = 0; j < NLD; ++j) {
+            const bool tok = 8 * (NLD * wave + j) < TM;  // uniform
+            lds_void* dst = reinterpret_cast<lds_void*>(reinterpret_cast<uintptr_t>(slot + 1024 * (NLD * wave + j)));
+            raw_buffer_load_lds(tok ? rtok : rw, dst, 16, static_cast<int>(voff[j]), st * kFp8Block, 0, 0);
+        }
+    };
+
+    // scales: a token row's per lane, one (SwiGLU: two) of the weights for the tile
+    const float* tsc[MI];
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) {
+        const int64_t pos = ti.row0 + std::min(mi * 16 + l16, ti.valid - 1);
+        tsc[mi] = p.a_scale + (p.row_index ? p.row_index[pos] : pos) * nkb;
+    }
+    const float* sg = p.b_scale + static_cast<int64_t>(ti.group) * scale_rows(p) * nkb;
+    const float* wsc0 = sg + static_cast<int64_t>(weight_row<TN, SWIGLU>(p, ti.nt, 0) / kFp8Block) * nkb;
+    const float* wsc1 = sg + static_cast<int64_t>(weight_row<TN, SWIGLU>(p, ti.nt, TN / 2) / kFp8Block) * nkb;
+
+    const int soff = (lg ^ swz(l16)) * 16, soff4 = ((4 + lg) ^ swz(l16)) * 16;  // blocks start at multiples of 16 rows
+    int foff_t[MI], foff_w[NI];
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) foff_t[mi] = (mi * 16 + l16) * kFp8Block;
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni)
+        foff_w[ni] = (TM + (SWIGLU ? ni * (TN / 2) + wave * 16 : wave * 32 + ni * 16) + l16) * kFp8Block;
+    f32x4 acc[NI][MI];
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni)
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) acc[ni][mi] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    float st_next[MI], sw_next[2];
+    auto load_scales = [&](int st) {
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) st_next[mi] = tsc[mi][st];
+        sw_next[0] = wsc0[st];
+        sw_next[1] = SWIGLU ? wsc1[st] : sw_next[0];
+    };
+    auto step = [&](int st, const char* cur, char* refill) {
+        if (st >= nkb) return;
+        // slabs issued after this one stay in flight
+        const int later = std::min(RING - 2, nkb - 1 - st);
+        if (RING == 4 && later >= 2) __builtin_amdgcn_s_waitcnt(vmcnt_imm(2 * NLD));
+        else if (later >= 1) __builtin_amdgcn_s_waitcnt(vmcnt_imm(NLD));
+        else __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+        // every wave's loads of this slab have landed, and every wave is done with the previous
+        // slab, whose slot is refilled next
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_barrier" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        float s[NI][MI];
+#pragma unroll
+        for (int ni = 0; ni < NI; ++ni)
+#pragma unroll
+            for (int mi = 0; mi < MI; ++mi) s[ni][mi] = st_next[mi] * sw_next[ni];
+        if (st + 1 < nkb) load_scales(st + 1);
+        if (st + RING - 1 < nkb) issue(st + RING - 1, refill);
+        i32x8 ft[MI], fw[NI];
+#pragma unroll
+        for (int ni = 0; ni < NI; ++ni)
+            fw[ni] = frag8(*reinterpret_cast<const uint4*>(cur + foff_w[ni] + soff),
+                           *reinterpret_cast<const uint4*>(cur + foff_w[ni] + soff4));
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi)
+            ft[mi] = frag8(*reinterpret_cast<const uint4*>(cur + foff_t[mi] + soff),
+                           *reinterpret_cast<const uint4*>(cur + foff_t[mi] + soff4));
+        auto add = [&](int ni, int mi, f32x4 part) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[ni][mi][i] = fmaf(part[i], s[ni][mi], acc[ni][mi][i]);
+        };
+        if constexpr (EXACT) {
+            Wide ww[NI];
+#pragma unroll
+            for (int ni = 0; ni < NI; ++ni) ww[ni] = widen(fw[ni]);
+#pragma unroll
+            for (int mi = 0; mi < MI; ++mi) {
+                const Wide wt = widen(ft[mi]);
+#pragma unroll
+                for (int ni = 0; ni < NI; ++ni) add(ni, mi, mfma_wide(ww[ni], wt));
+            }
+        } else {
+#pragma unroll
+            for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+                for (int ni = 0; ni < NI; ++ni) add(ni, mi, mfma8(fw[ni], ft[mi]));
+        }
+    };
+    load_scales(0);
+    issue(0, lds0);
+    if (nkb > 1) issue(1, lds1);
+    if (RING == 4 && nkb > 2) issue(2, lds2);
+    for (int st = 0; st < nkb; st += RING) {
+        if constexpr (RING == 3) {
+            step(st, lds0, lds2);
+            step(st + 1, lds1, lds0);
+            step(st + 2, lds2, lds1);
+        } else {
+            step(st, lds0, lds3);
+            step(st + 1, lds1, lds0);
+            step(st + 2, lds2, lds1);
+            step(st + 3, lds3, lds2);
+        }
+    }
+    TO* out = static_cast<TO*>(p.out);
+    const bool runs = p.N % 4 == 0;
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) {
+        const int r = mi * 16 + l16;
+        if (r >= ti.valid) continue;
+        TO* orow = out + (ti.row0 + r) * p.N;
+#pragma unroll
+        for (int ni = 0; ni < (SWIGLU ? 1 : NI); ++ni) {
+            const int c = ti.nt * NOUT + (SWIGLU ? wave * 16 : wave * 32 + ni * 16) + 4 * lg;
+            f32x4 v = acc[ni][mi];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (SWIGLU) v[i] = silu(v[i]) * acc[NI - 1][mi][i];
+                else if (EPI == Epilogue::ReLU) v[i] = relu(v[i]);
+            }
+            if (c < p.N) store_run(orow + c, v, p.N - c, c + 4 <= p.N && runs);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ 256 x 256 tiles
+//
+// Waves 0-3 (group 0, token loaders) and waves 4-7 (group 1, weight loaders) sit one per SIMD each; the
+// groups alternate between a compute phase (the 32 products of one slab of 128 k, at raised priority) and a
+// memory phase (fragment reads of the next slab, buffer loads), with a workgroup barrier between phases, so on
+// every SIMD one wave issues products while the other waits on memory.
+//   group 0, slab s: issue token rows of slab s+1 | read slab s | barrier | products of slab s |
+//                    wait own loads | barrier
+//   group 1, slab s: products of slab s-1 | barrier | issue weight rows of slab s+2 into the slot of
+//                    slab s-1, read slab s | wait loads of slab s+1 | barrier
+// Token rows sit in two 32 KB slots and weight rows in three, so that every slot is refilled only after a
+// barrier that follows the last read of it by any wave. A wave holds 4 x 8 blocks of 16 x 16 (128 float32
+// sums). The memory phase reads the token fragments and the first two weight blocks' fragments; a weight
+// block's 32 bytes a lane are read two blocks of products ahead, behind the same barriers. The scales of slab s are
+// loaded in its memory phase, ahead of the slab loads, so the counted waits cover them. The 128
+// scaling multiply-adds of a slab issue under its products (16 of every 32 cycles).
+// EPI Store writes bfloat16 rows. SwiGLU and ReLU quantise: a tile holds one (ReLU: two) whole blocks of 128
+// hidden columns of each row, whose largest value meets across the lanes and, with SwiGLU, the two
+// waves of the row.
+template <Epilogue EPI>
+__global__ __launch_bounds__(512, 1) void fp8_pp_kernel(Fp8GemmArgs p) {
+    constexpr bool SWIGLU = EPI == Epilogue::SwiGLU;
+    constexpr bool QUANT = EPI != Epilogue::Store;
+    constexpr int TM = 256, TN = 256, WM = 4, WN = 2, NW = 8;
+    constexpr int MI = TM / WM / 16;           // 4 token blocks of 16 per wave
+    constexpr int NI = TN / WN / 16;           // 8 weight blocks of 16 per wave
+    constexpr int NOUT = SWIGLU ? TN / 2 : TN;
+    constexpr int RB = kFp8Block;
+    constexpr int SLOT = TM * RB;              // 32 KB: the token rows, or the weight rows, of one slab
+    constexpr int WROWS = (TM + TN) / NW;      // 64 rows a wave loads
+    constexpr int LOADS = WROWS / 8;           // 8
+    constexpr int WTOK = TM / WM;
+
+    __shared__ __attribute__((aligned(1024))) char t0[SLOT];
+    __shared__ __attribute__((aligned(1024))) char t1[SLOT];
+    __shared__ __attribute__((aligned(1024))) char w0[SLOT];
+    __shared__ __attribute__((aligned(1024))) char w1[SLOT];
+    __shared__ __attribute__((aligned(1024))) char w2[SLOT];
+
+    const int ntn = (p.N + NOUT - 1) / NOUT;
+    const int K = p.K, nk = K / kFp8Block;
+    constexpr int P = 256;           // workgroups, one per CU
+    constexpr int XW = P / kXcds;
+    const int total = count_tiles<TM>(p, ntn);
+    const int rounds = total / P;
+    const int wg = blockIdx.x;
+
+    // whole rounds first, each XCD's workgroups stepping through consecutive tiles; then the tail
+    for (int it = 0; it <= rounds; ++it) {
+    int bid;
+    if (it < rounds) {
+        bid = (wg % kXcds) * (rounds * XW) + it * XW + wg / kXcds;
+    } else {
+        bid = rounds * P + wg;
+        if (bid >= total) break;
+    }
+    TileInfo ti;
+    if (!tile_of<TM>(p, ntn, bid, ti)) break;
+
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    const int lane = tid & 63;
+    const int wave = uniform(tid >> 6);
+    const int wm = wave % WM;
+    const int wn = wave / WM;                 // also the group
+    const bool tok_wave = wave * WROWS < TM;  // group 0
+    const uint8_t* abase = p.row_index ? p.a : p.a + ti.row0 * K;
+    const uint8_t* bbase = p.b + static_cast<int64_t>(ti.group) * p.b_rows * K;
+    const i32x4 rs = tok_wave ? buffer_rsrc(abase, static_cast<uint32_t>(p.row_index ? p.src_rows * K : static_cast<int64_t>(ti.valid) * K))
+                              : buffer_rsrc(bbase, static_cast<uint32_t>(static_cast<int64_t>(p.b_rows) * K));
+    uint32_t voff[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        const int row = wave * WROWS + i * 8 + (lane >> 3);
+        uint32_t src;
+        if (tok_wave) {
+            const int r = std::min(row, ti.valid - 1);
+            src = p.row_index ? static_cast<uint32_t>(p.row_index[ti.row0 + r]) : static_cast<uint32_t>(r);
+        } else {
+            src = static_cast<uint32_t>(weight_row<TN, SWIGLU>(p, ti.nt, row - TM));
+        }
+        voff[i] = src * static_cast<uint32_t>(K) + static_cast<uint32_t>(((lane & 7) ^ ((row >> 1) & 7)) * 16);
+        asm volatile("" : "+v"(voff[i]));  // kept as it is: the compiler would hold the 64-bit product
+    }
+    // this wave's rows of a slab into a token or weight slot (rows 64 (wave & 3) .. + 63 of it)
+    auto issue_slab = [&](int ks, char* slot) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            lds_void* dst = reinterpret_cast<lds_void*>(
+                reinterpret_cast<uintptr_t>(slot + ((wave & 3) * WROWS + i * 8) * RB));
+            raw_buffer_load_lds(rs, dst, 16, static_cast<int>(voff[i]), ks * RB, 0, 0);
+        }
+    };
+
+    const int l16 = lane & 15;
+    const int lg = lane >> 4;
+    const int sw = (l16 >> 1) & 7;
+    constexpr int WW = SWIGLU ? TN / 2 / WN : TN / WN;
+    const int c0 = (lg ^ sw) * 16, c1 = ((4 + lg) ^ sw) * 16;
+    const int off_t = (wm * WTOK + l16) * RB;  // in a token slot
+    const int off_w = (wn * WW + l16) * RB;    // in a weight slot
+    auto wblk = [](int ni) constexpr {
+        if (SWIGLU) {
+            constexpr int HALF = NI / 2;
+            return (ni < HALF ? 0 : TN / 2) + (ni % HALF) * 16;
+        }
+        return ni * 16;
+    };
+
+    // scales: of the lane's four token rows, and of the wave's weight block (SwiGLU: gate and up)
+    uint32_t tso[MI];
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) {
+        const int64_t pos = ti.row0 + std::min(wm * WTOK + mi * 16 + l16, ti.valid - 1);
+        tso[mi] = static_cast<uint32_t>(p.row_index ? p.row_index[pos] : pos) * static_cast<uint32_t>(4 * nk);
+        asm volatile("" : "+v"(tso[mi]));
+    }
+    const float* sg = p.b_scale + static_cast<int64_t>(ti.group) * scale_rows(p) * nk;
+    // (read through the scalar cache: uniform, and written by no kernel that runs now)
+    const cfloat* ws0 = (const cfloat*)(sg + static_cast<int64_t>(uniform(weight_row<TN, SWIGLU>(p, ti.nt, wn * WW) / kFp8Block)) * nk);
+    const cfloat* ws1 =
+        (const cfloat*)(sg + static_cast<int64_t>(uniform(weight_row<TN, SWIGLU>(p, ti.nt, TN / 2 + wn * WW) / kFp8Block)) * nk);
+    struct Scales {
+        float t[MI], w0, w1;
+    };
+    auto load_scales = [&](int ks, Scales& s) {
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi)
+            s.t[mi] = *reinterpret_cast<const float*>(reinterpret_cast<const char*>(p.a_scale + ks) + tso[mi]);
+        s.w0 = ws0[ks];
+        s.w1 = SWIGLU ? ws1[ks] : 0.f;
+    };
+
+    f32x4 acc[NI][MI];
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni)
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) acc[ni][mi] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    constexpr int AHEAD = 2;
+    struct Frags {
+        i32x8 a[AHEAD], b[MI];
+    };
+    auto read_w = [&](const char* wslot, int ni) {
+        return frag8(*reinterpret_cast<const uint4*>(wslot + off_w + c0 + wblk(ni) * RB),
+                     *reinterpret_cast<const uint4*>(wslot + off_w + c1 + wblk(ni) * RB));
+    };
+    auto read_slab = [&](const char* tslot, const char* wslot, Frags& f) {
+#pragma unroll
+        for (int ni = 0; ni < AHEAD; ++ni) f.a[ni] = read_w(wslot, ni);
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi)
+            f.b[mi] = frag8(*reinterpret_cast<const uint4*>(tslot + off_t + c0 + mi * 16 * RB),
+                           *reinterpret_cast<const uint4*>(tslot + off_t + c1 + mi * 16 * RB));
+    };
+    auto mma_slab = [&](const char* wslot, Frags& f, const Scales& s) {
+        __builtin_amdgcn_s_setprio(1);
+        float sc[SWIGLU ? 2 : 1][MI];
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) {
+            sc[0][mi] = s.t[mi] * s.w0;
+            if (SWIGLU) sc[SWIGLU ? 1 : 0][mi] = s.t[mi] * s.w1;
+        }
+        // two products, then the multiply-adds of the two before, in this order: left alone the scheduler
+        // raises all products of the slab above them and spills
+        constexpr int NP = NI * MI / 2;
+        f32x4 part[2][2];
+        auto add = [&](int q) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int ni = q * 2 / MI, mi = q * 2 % MI + h;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    acc[ni][mi][i] = fmaf(part[q & 1][h][i], sc[SWIGLU && ni >= NI / 2 ? 1 : 0][mi], acc[ni][mi][i]);
+            }
+        };
+#pragma unroll
+        for (int q = 0; q < NP; ++q) {
+            const int ni = q * 2 / MI;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) part[q & 1][h] = mfma8(f.a[ni % AHEAD], f.b[q * 2 % MI + h]);
+            if (q * 2 % MI == MI - 2 && ni + AHEAD < NI) f.a[ni % AHEAD] = read_w(wslot, ni + AHEAD);
+            if (q > 0) add(q - 1);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        add(NP - 1);
+        // the sums are wanted here: the compiler otherwise sinks the multiply-adds past the barrier, into the next
+        // phase, and spills the products
+#pragma unroll
+        for (int ni = 0; ni < NI; ++ni)
+#pragma unroll
+            for (int mi = 0; mi < MI; ++mi) asm volatile("" : "+v"(acc[ni][mi]));
+        __builtin_amdgcn_s_setprio(0);
+    };
+    auto barrier = [&]() {
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_barrier" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
+    // slab s: tokens in slot s % 2, weights in slot s % 3 (the loops run six slabs a turn)
+    if (tok_wave) {
+        issue_slab(0, t0);
+        __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+        barrier();
+        auto slab0 = [&](const char* tcur, char* tnxt, const char* wcur, int s) {
+            Scales sc;
+            Frags f;
+            load_scales(s, sc);
+            __builtin_amdgcn_sched_barrier(0);
+            if (s + 1 < nk) issue_slab(s + 1, tnxt);
+            read_slab(tcur, wcur, f);
+            __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+            barrier();
+            mma_slab(wcur, f, sc);
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_waitcnt(0x0070);  // token rows of slab s+1 landed
+            barrier();
+        };
+        int s = 0;
+        for (; s + 6 <= nk; s += 6) {
+            slab0(t0, t1, w0, s);
+            slab0(t1, t0, w1, s + 1);
+            slab0(t0, t1, w2, s + 2);
+            slab0(t1, t0, w0, s + 3);
+            slab0(t0, t1, w1, s + 4);
+            slab0(t1, t0, w2, s + 5);
+        }
+        if (s < nk) slab0(t0, t1, w0, s);
+        if (s + 1 < nk) slab0(t1, t0, w1, s + 1);
+        if (s + 2 < nk) slab0(t0, t1, w2, s + 2);
+        if (s + 3 < nk) slab0(t1, t0, w0, s + 3);
+        if (s + 4 < nk) slab0(t0, t1, w1, s + 4);
+    } else {
+        Scales sc;
+        Frags f;
+        issue_slab(0, w0);
+        issue_slab(1, w1);  // nk >= 2 on this path
+        __builtin_amdgcn_s_waitcnt(vmcnt_imm(LOADS));  // own rows of slab 0 landed
+        barrier();
+        // Memory phase of slab s. The slot refilled in it holds slab s - 1, whose last reads (this group's) were
+        // done before the barrier ahead of it: no wave can still be reading it.
+        auto fetch = [&](const char* tcur, const char* wcur, char* wfree, int s) {
+            barrier();
+            load_scales(s, sc);
+            __builtin_amdgcn_sched_barrier(0);
+            if (s + 2 < nk) issue_slab(s + 2, wfree);
+            read_slab(tcur, wcur, f);
+            __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+            if (s + 2 < nk) __builtin_amdgcn_s_waitcnt(vmcnt_imm(LOADS));  // weight rows of slab s+1 landed
+            else __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+            barrier();
+        };
+        auto slab1 = [&](const char* tcur, const char* wcur, char* wfree, int s) {
+            mma_slab(wfree, f, sc);  // slab s - 1, whose weights sit in the slot refilled next
+            fetch(tcur, wcur, wfree, s);
+        };
+        fetch(t0, w0, w2, 0);
+        int s = 1;
+        for (; s + 6 <= nk; s += 6) {
+            slab1(t1, w1, w0, s);
+            slab1(t0, w2, w1, s + 1);
+            slab1(t1, w0, w2, s + 2);
+            slab1(t0, w1, w0, s + 3);
+            slab1(t1, w2, w1, s + 4);
+            slab1(t0, w0, w2, s + 5);
+        }
+        if (s < nk) slab1(t1, w1, w0, s);
+        if (s + 1 < nk) slab1(t0, w2, w1, s + 1);
+        if (s + 2 < nk) slab1(t1, w0, w2, s + 2);
+        if (s + 3 < nk) slab1(t0, w1, w0, s + 3);
+        if (s + 4 < nk) slab1(t1, w2, w1, s + 4);
+        const int last = (nk - 1) % 3;
+        mma_slab(last == 0 ? w0 : last == 1 ? w1 : w2, f, sc);
+    }
+
+    // The finished tile is staged in LDS so that the global stores are whole rows: 16 bytes per lane. Token
+    // slots are free after the last slab; weight slots once the weight loaders' last products are done.
+    if constexpr (QUANT) {
+        // Staged row r (NOUT bytes) holds its 16-byte chunk c at c ^ (r % OCH).
+        constexpr int OCH = NOUT / 16;
+        constexpr int NB = SWIGLU ? NI / 2 : NI;
+        uint32_t mx[MI];
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) {
+            mx[mi] = 0;
+#pragma unroll
+            for (int ni = 0; ni < NB; ++ni)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float v = SWIGLU ? silu(acc[ni][mi][e]) * acc[SWIGLU ? ni + NB : ni][mi][e] : relu(acc[ni][mi][e]);
+                    acc[ni][mi][e] = v;
+                    mx[mi] = max(mx[mi], magnitude(v));
+                }
+            mx[mi] = max(mx[mi], static_cast<uint32_t>(__shfl_xor(static_cast<int>(mx[mi]), 16)));
+            mx[mi] = max(mx[mi], static_cast<uint32_t>(__shfl_xor(static_cast<int>(mx[mi]), 32)));
+        }
+        if constexpr (SWIGLU) {
+            uint32_t* rowmax = reinterpret_cast<uint32_t*>(t1);  // [2][256]
+            if (lg == 0)
+#pragma unroll
+                for (int mi = 0; mi < MI; ++mi) rowmax[wn * TM + wm * WTOK + mi * 16 + l16] = mx[mi];
+            __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+            barrier();
+#pragma unroll
+            for (int mi = 0; mi < MI; ++mi) mx[mi] = max(mx[mi], rowmax[(1 - wn) * TM + wm * WTOK + mi * 16 + l16]);
+        }
+        const int nsb = p.N / kFp8Block;
+        const int blk = ti.nt * (NOUT / kFp8Block) + (SWIGLU ? 0 : wn);
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) {
+            const int r = wm * WTOK + mi * 16 + l16;
+            const BlockScale bs = block_scale(mx[mi]);
+            if ((SWIGLU ? wn == 0 : true) && lg == 0 && r < ti.valid && blk < nsb)
+                p.out_scale[(ti.row0 + r) * nsb + blk] = bs.scale;
+            char* row = (SWIGLU || r < 128 ? t0 : t1) + (SWIGLU ? r : r & 127) * NOUT;
+#pragma unroll
+            for (int ni = 0; ni < NB; ++ni) {
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = acc[ni][mi][e];
+                const int ch = (wn * (NOUT / WN / 16) + ni) ^ (r % OCH);
+                *reinterpret_cast<uint32_t*>(row + ch * 16 + 4 * lg) = quantize4(v, bs);
+            }
+        }
+        __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+        barrier();
+        constexpr int RPI = 64 / OCH;
+        uint8_t* out = static_cast<uint8_t*>(p.out);
+#pragma unroll
+        for (int j = 0; j < TM / NW / RPI; ++j) {
+            const int r = wave * (TM / NW) + j * RPI + lane / OCH;
+            const int c = lane % OCH;
+            const char* src = (SWIGLU || r < 128 ? t0 : t1) + (SWIGLU ? r : r & 127) * NOUT + ((c ^ (r % OCH)) * 16);
+            const uint4 v = *reinterpret_cast<const uint4*>(src);
+            const int col = ti.nt * NOUT + c * 16;
+            if (r < ti.valid && col < p.N) *reinterpret_cast<uint4*>(out + (ti.row0 + r) * p.N + col) = v;
+        }
+    } else {
+        constexpr int OROW = NOUT * 2;   // bytes per staged row
+        constexpr int OCH = OROW / 16;   // 16-byte chunks per row
+        constexpr int RPS = SLOT / OROW;  // rows per 32 KB slot: 64
+        static_assert(TM <= 4 * RPS && WTOK <= RPS && RPS % WTOK == 0, "staged tile fits four slots");
+        auto ost = [&](int i) -> char* { return i == 0 ? t0 : i == 1 ? t1 : i == 2 ? w0 : w1; };
+        char* wst = ost(wm * WTOK / RPS) + (wm * WTOK % RPS) * OROW;
+        barrier();  // the weight loaders' last products read a weight slot
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) {
+            const int r = mi * 16 + l16;
+            const int sr = wm * WTOK + r;
+#pragma unroll
+            for (int ni = 0; ni < NI; ++ni) {
+                bf16x4 o;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = static_cast<__bf16>(acc[ni][mi][e]);
+                const int col = wn * (NOUT / WN) + ni * 16 + 8 * (lg >> 1);
+                const int ch = (col / 8) ^ (sr % OCH);
+                *reinterpret_cast<bf16x4*>(wst + r * OROW + ch * 16 + (lg & 1) * 8) = o;
+            }
+        }
+        __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+        barrier();
+        constexpr int RPI = 64 / OCH;
+        bf16_t* out = static_cast<bf16_t*>(p.out);
+#pragma unroll
+        for (int j = 0; j < TM / NW / RPI; ++j) {
+            const int r = wave * (TM / NW) + j * RPI + lane / OCH;
+            const int c = lane % OCH;
+            const char* src = ost(r / RPS) + (r % RPS) * OROW + ((c ^ (r % OCH)) * 16);
+            const uint4 v = *reinterpret_cast<const uint4*>(src);
+            const int col = ti.nt * NOUT + c * 8;
+            if (r < ti.valid && col < p.N) *reinterpret_cast<uint4*>(out + (ti.row0 + r) * p.N + col) = v;
+        }
+    }
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): staged rows read before the slots refill
+    barrier();
+    }
+}
+
+// ------------------------------------------------------------------ dispatch
+
 // Tiles of a launch at most: a group of r rows has ceil(r / TM) <= r / TM + 1 of them per column tile.
 int64_t max_tiles(const Fp8GemmArgs& a, int tm, int tn) {
     const int64_t mt = a.seg ? a.rows / tm + std::min<int64_t>(a.rows, a.n_groups) : (a.rows + tm - 1) / tm;
     return mt * ((a.N + tn - 1) / tn);
 }
 
+unsigned tile_grid(const Fp8GemmArgs& a, int tm, int tn) {
+    return static_cast<unsigned>((max_tiles(a, tm, tn) + kXcds - 1) / kXcds * kXcds);
+}
+
 template <typename TO, int MT, int NT, int WAVES, Epilogue EPI>
 hipError_t run_skinny(const Fp8GemmArgs& a, hipStream_t s) {
-    const int64_t grid = (max_tiles(a, 16 * MT, 16 * NT) + kXcds - 1) / kXcds * kXcds;
-    if (grid == 0) return hipSuccess;
     ProfileScope prof(a.name, s);
-    hipLaunchKernelGGL((fp8_skinny_kernel<TO, MT, NT, WAVES, EPI>), dim3(static_cast<unsigned>(grid)), dim3(64 * WAVES), 0, s,
-                       a);
+    hipLaunchKernelGGL((fp8_skinny_kernel<TO, MT, NT, WAVES, EPI>), dim3(tile_grid(a, 16 * MT, 16 * NT)), dim3(64 * WAVES), 0,
+                       s, a);
     return hipGetLastError();
 }
 
-template <typename TO, Epilogue EPI>
-hipError_t dispatch(const Fp8GemmArgs& a, hipStream_t s) {
+template <typename TO, int TM, int RING, Epilogue EPI, bool EXACT>
+hipError_t run_ring(const Fp8GemmArgs& a, hipStream_t s) {
+    ProfileScope prof(a.name, s);
+    hipLaunchKernelGGL((fp8_ring_kernel<TO, TM, RING, EPI, EXACT>), dim3(tile_grid(a, TM, EPI == Epilogue::SwiGLU ? 64 : 128)),
+                       dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+template <Epilogue EPI>
+hipError_t run_pp(const Fp8GemmArgs& a, hipStream_t s) {
+    ProfileScope prof(a.name, s);
+    hipLaunchKernelGGL((fp8_pp_kernel<EPI>), dim3(256), dim3(512), 0, s, a);
+    return hipGetLastError();
+}
+
+int64_t avg_rows(const Fp8GemmArgs& a) { return a.rows / std::max(1, a.n_groups); }
+
+// 32-bit byte offsets of gathered token rows and of scale rows
+bool offsets32(const Fp8GemmArgs& a) {
+    return (!a.row_index || a.src_rows * a.K < (int64_t(1) << 32)) && a.src_rows * (a.K / kFp8Block) * 4 < (int64_t(1) << 32);
+}
+
+bool use_pp(const Fp8GemmArgs& a) {
+    return offsets32(a) && avg_rows(a) >= 256 && a.K >= 2 * kFp8Block;
+}
+
+template <typename TO, Epilogue EPI, bool EXACT>
+hipError_t dispatch_small(const Fp8GemmArgs& a, hipStream_t s) {
     constexpr int NT = EPI == Epilogue::SwiGLU ? 2 : 4;
-    if (a.rows / std::max(1, a.n_groups) >= 16) return run_skinny<TO, 4, NT, 4, EPI>(a, s);
-    return run_skinny<TO, 1, NT, 4, EPI>(a, s);
+    if (avg_rows(a) < 16 || !offsets32(a)) return run_skinny<TO, 1, NT, 4, EPI>(a, s);
+    return run_ring<TO, 64, 3, EPI, EXACT>(a, s);
 }
 
 }  // namespace
@@ -175,13 +779,32 @@ bool fp8_gemm_fits(int64_t rows, int n_groups, int64_t n) {
     return max_tiles(a, 16, 32) < (int64_t(1) << 23);  // workgroups of 256 threads of a launch: 2^32 threads at most
 }
 
-hipError_t launch_fp8_gemm(Epilogue epi, DType out_type, const Fp8GemmArgs& a, hipStream_t s) {
-    const bool f32 = out_type == DType::F32;
-    switch (epi) {
-        case Epilogue::SwiGLU: return dispatch<float, Epilogue::SwiGLU>(a, s);
-        case Epilogue::ReLU: return dispatch<float, Epilogue::ReLU>(a, s);
-        default: return f32 ? dispatch<float, Epilogue::Store>(a, s) : dispatch<bf16_t, Epilogue::Store>(a, s);
-    }
+hipError_t launch_fp8_gemm(DType out_type, const Fp8GemmArgs& a, hipStream_t s) {
+    if (a.rows == 0) return hipSuccess;
+    if (out_type == DType::F32) return dispatch_small<float, Epilogue::Store, true>(a, s);
+    if (use_pp(a) && a.N % 8 == 0) return run_pp<Epilogue::Store>(a, s);
+    return dispatch_small<bf16_t, Epilogue::Store, false>(a, s);
+}
+
+size_t fp8_hidden_scratch_bytes(Epilogue, int64_t rows, int n_groups, int K, int N) {
+    Fp8GemmArgs a{};
+    a.rows = rows;
+    a.n_groups = n_groups;
+    a.K = K;
+    a.N = N;
+    return use_pp(a) ? 0 : static_cast<size_t>(rows) * N * sizeof(float);
+}
+
+hipError_t launch_fp8_hidden(Epilogue epi, const Fp8GemmArgs& a, float* scratch, hipStream_t s) {
+    if (a.rows == 0) return hipSuccess;
+    const bool swiglu = epi == Epilogue::SwiGLU;
+    if (use_pp(a)) return swiglu ? run_pp<Epilogue::SwiGLU>(a, s) : run_pp<Epilogue::ReLU>(a, s);
+    Fp8GemmArgs g = a;
+    g.out = scratch;
+    const hipError_t e = swiglu ? dispatch_small<float, Epilogue::SwiGLU, false>(g, s)
+                                : dispatch_small<float, Epilogue::ReLU, false>(g, s);
+    if (e != hipSuccess) return e;
+    return launch_fp8_quantize(DType::F32, scratch, 1, static_cast<int>(a.rows), a.N, 1, a.out, a.out_scale, s);
 }
 
 }  // namespace ec2moe

@@ -14,43 +14,10 @@
 // orders like the magnitudes with infinity and NaN above them.
 #include "device_common.h"
 #include "fp8.h"
+#include "fp8_device.h"
 
 namespace ec2moe {
 namespace {
-
-constexpr float kFp8Max = 448.f;
-constexpr uint32_t kAmaxMin = 0x0d800000u;  // 2^-100
-
-struct BlockScale {
-    float scale, amax, rcp, mul;  // mul: 448, or a power of two less for blocks where 448 x overflows
-    bool finite;
-};
-
-__device__ __forceinline__ BlockScale block_scale(uint32_t amax_bits) {
-    BlockScale b;
-    b.finite = amax_bits < 0x7f800000u;
-    float amax = __uint_as_float(max(amax_bits, kAmaxMin));
-    b.scale = b.finite ? amax / kFp8Max : __uint_as_float(0x7fc00000u);
-    const bool big = amax_bits >= 0x71800000u;  // 2^100
-    b.amax = big ? amax * 0x1p-32f : amax;
-    b.mul = big ? kFp8Max * 0x1p-32f : kFp8Max;
-    b.rcp = 1.0f / b.amax;
-    return b;
-}
-
-__device__ __forceinline__ float quotient(float x, const BlockScale& b) {
-    const float n = x * b.mul;
-    const float t = n * b.rcp;
-    return fmaf(b.rcp, fmaf(-t, b.amax, n), t);
-}
-
-// four values to four bytes
-__device__ __forceinline__ uint32_t quantize4(const float* x, const BlockScale& b) {
-    int w = 0;
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(x[0], b), quotient(x[1], b), w, false);
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(x[2], b), quotient(x[3], b), w, true);
-    return b.finite ? static_cast<uint32_t>(w) : 0x7f7f7f7fu;
-}
 
 // 8 consecutive values as loaded: one or two 16-byte chunks
 template <typename T>
