@@ -343,9 +343,9 @@ __global__ __launch_bounds__(256, 2) void fp8_ring_kernel(Fp8GemmArgs p) {
 //                    slab s-1, read slab s | wait loads of slab s+1 | barrier
 // Token rows sit in two 32 KB slots and weight rows in three, so that every slot is refilled only after a
 // barrier that follows the last read of it by any wave. A wave holds 4 x 8 blocks of 16 x 16 (128 float32
-// sums). The memory phase reads the token fragments and the first two weight blocks' fragments; a weight
-// block's 32 bytes a lane are read two blocks of products ahead, behind the same barriers. The scales of slab s are
-// loaded in its memory phase, ahead of the slab loads, so the counted waits cover them. The 128
+// sums). The memory phase reads the token fragments and the first weight blocks' fragments; a weight
+// block's 32 bytes a lane are read AHEAD blocks of products ahead, behind the same barriers. Scales are loaded a slab
+// ahead and before the slab loads of the phase, so that its counted waits cover them. The 128
 // scaling multiply-adds of a slab issue under its products (16 of every 32 cycles).
 // EPI Store writes bfloat16 rows. SwiGLU and ReLU quantise: a tile holds one (ReLU: two) whole blocks of 128
 // hidden columns of each row, whose largest value meets across the lanes and, with SwiGLU, the two
@@ -440,28 +440,40 @@ __global__ __launch_bounds__(512, 1) void fp8_pp_kernel(Fp8GemmArgs p) {
         return ni * 16;
     };
 
-    // scales: of the lane's four token rows, and of the wave's weight block (SwiGLU: gate and up)
-    uint32_t tso[MI];
-#pragma unroll
-    for (int mi = 0; mi < MI; ++mi) {
-        const int64_t pos = ti.row0 + std::min(wm * WTOK + mi * 16 + l16, ti.valid - 1);
-        tso[mi] = static_cast<uint32_t>(p.row_index ? p.row_index[pos] : pos) * static_cast<uint32_t>(4 * nk);
-        asm volatile("" : "+v"(tso[mi]));
+    // Scales: a lane loads the one of row `lane` of the wave's 64 token rows, a slab ahead; those of the wave's
+    // weight block (SwiGLU: gate and up) are uniform and come through the scalar cache (written by no kernel that
+    // runs now).
+    uint32_t tso;
+    {
+        const int64_t pos = ti.row0 + std::min(wm * WTOK + lane, ti.valid - 1);
+        tso = static_cast<uint32_t>(p.row_index ? p.row_index[pos] : pos) * static_cast<uint32_t>(4 * nk);
+        asm volatile("" : "+v"(tso));
     }
     const float* sg = p.b_scale + static_cast<int64_t>(ti.group) * scale_rows(p) * nk;
-    // (read through the scalar cache: uniform, and written by no kernel that runs now)
     const cfloat* ws0 = (const cfloat*)(sg + static_cast<int64_t>(uniform(weight_row<TN, SWIGLU>(p, ti.nt, wn * WW) / kFp8Block)) * nk);
     const cfloat* ws1 =
         (const cfloat*)(sg + static_cast<int64_t>(uniform(weight_row<TN, SWIGLU>(p, ti.nt, TN / 2 + wn * WW) / kFp8Block)) * nk);
     struct Scales {
-        float t[MI], w0, w1;
+        float t, w0, w1;
     };
-    auto load_scales = [&](int ks, Scales& s) {
-#pragma unroll
-        for (int mi = 0; mi < MI; ++mi)
-            s.t[mi] = *reinterpret_cast<const float*>(reinterpret_cast<const char*>(p.a_scale + ks) + tso[mi]);
+    auto load_scales = [&](int ks) {
+        Scales s;
+        s.t = *reinterpret_cast<const float*>(reinterpret_cast<const char*>(p.a_scale + ks) + tso);
         s.w0 = ws0[ks];
         s.w1 = SWIGLU ? ws1[ks] : 0.f;
+        return s;
+    };
+    // out[mi] of every lane = v of lane 16 mi + l16
+    auto spread = [&](float v, float (&out)[MI]) {
+        typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+        const uint32_t u = __float_as_uint(v);
+        const u32x2 r = __builtin_amdgcn_permlane16_swap(u, u, false, false);    // rows 0 0 2 2, 1 1 3 3
+        const u32x2 e = __builtin_amdgcn_permlane32_swap(r[0], r[0], false, false);  // rows 0 0 0 0, 2 2 2 2
+        const u32x2 o = __builtin_amdgcn_permlane32_swap(r[1], r[1], false, false);
+        out[0] = __uint_as_float(e[0]);
+        out[1] = __uint_as_float(o[0]);
+        out[2] = __uint_as_float(e[1]);
+        out[3] = __uint_as_float(o[1]);
     };
 
     f32x4 acc[NI][MI];
@@ -489,11 +501,8 @@ __global__ __launch_bounds__(512, 1) void fp8_pp_kernel(Fp8GemmArgs p) {
     auto mma_slab = [&](const char* wslot, Frags& f, const Scales& s) {
         __builtin_amdgcn_s_setprio(1);
         float sc[SWIGLU ? 2 : 1][MI];
-#pragma unroll
-        for (int mi = 0; mi < MI; ++mi) {
-            sc[0][mi] = s.t[mi] * s.w0;
-            if (SWIGLU) sc[SWIGLU ? 1 : 0][mi] = s.t[mi] * s.w1;
-        }
+        spread(s.t * s.w0, sc[0]);
+        if (SWIGLU) spread(s.t * s.w1, sc[SWIGLU ? 1 : 0]);
         // two products, then the multiply-adds of the two before, in this order: left alone the scheduler
         // raises all products of the slab above them and spills
         constexpr int NP = NI * MI / 2;
@@ -537,13 +546,14 @@ __global__ __launch_bounds__(512, 1) void fp8_pp_kernel(Fp8GemmArgs p) {
 
     // slab s: tokens in slot s % 2, weights in slot s % 3 (the loops run six slabs a turn)
     if (tok_wave) {
+        Scales nxt = load_scales(0);
         issue_slab(0, t0);
         __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
         barrier();
         auto slab0 = [&](const char* tcur, char* tnxt, const char* wcur, int s) {
-            Scales sc;
             Frags f;
-            load_scales(s, sc);
+            const Scales sc = nxt;
+            nxt = load_scales(std::min(s + 1, nk - 1));
             __builtin_amdgcn_sched_barrier(0);
             if (s + 1 < nk) issue_slab(s + 1, tnxt);
             read_slab(tcur, wcur, f);
@@ -569,8 +579,9 @@ __global__ __launch_bounds__(512, 1) void fp8_pp_kernel(Fp8GemmArgs p) {
         if (s + 3 < nk) slab0(t1, t0, w0, s + 3);
         if (s + 4 < nk) slab0(t0, t1, w1, s + 4);
     } else {
-        Scales sc;
+        Scales sc, nxt = load_scales(0);
         Frags f;
+        __builtin_amdgcn_sched_barrier(0);
         issue_slab(0, w0);
         issue_slab(1, w1);  // nk >= 2 on this path
         __builtin_amdgcn_s_waitcnt(vmcnt_imm(LOADS));  // own rows of slab 0 landed
@@ -579,13 +590,18 @@ __global__ __launch_bounds__(512, 1) void fp8_pp_kernel(Fp8GemmArgs p) {
         // done before the barrier ahead of it: no wave can still be reading it.
         auto fetch = [&](const char* tcur, const char* wcur, char* wfree, int s) {
             barrier();
-            load_scales(s, sc);
-            __builtin_amdgcn_sched_barrier(0);
+            sc = nxt;
             if (s + 2 < nk) issue_slab(s + 2, wfree);
+            __builtin_amdgcn_sched_barrier(0);
+            // after the slab loads: the wait below then leaves it in flight (a load's latency a slab otherwise:
+            // gate-up of the layer of 8 experts 1007 us, 967 so)
+            nxt = load_scales(std::min(s + 1, nk - 1));
+            __builtin_amdgcn_sched_barrier(0);
             read_slab(tcur, wcur, f);
             __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
-            if (s + 2 < nk) __builtin_amdgcn_s_waitcnt(vmcnt_imm(LOADS));  // weight rows of slab s+1 landed
-            else __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+            // weight rows of slab s+1 landed
+            if (s + 2 < nk) __builtin_amdgcn_s_waitcnt(vmcnt_imm(LOADS + 1));
+            else __builtin_amdgcn_s_waitcnt(vmcnt_imm(1));
             barrier();
         };
         auto slab1 = [&](const char* tcur, const char* wcur, char* wfree, int s) {
