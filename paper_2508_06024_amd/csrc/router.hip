@@ -14,7 +14,7 @@ constexpr int kMaxGroups = 160;
 // names of the timing record (launches outside the layer step)
 constexpr const char *kBalanceName = "balance_loss", *kBalanceFinishName = "balance_finish",
                      *kLogitGradName = "gate_logit_grad", *kDxName = "gate_dx", *kDwName = "gate_dw",
-                     *kDbName = "gate_db", *kDwSumName = "gate_dw_sum";
+                     *kDwSumName = "gate_dw_sum";
 
 // ------------------------------------------------------------------ load balance loss
 //
@@ -154,265 +154,527 @@ __global__ __launch_bounds__(1024) void balance_finish_kernel(BalanceArgs a, int
 
 // ------------------------------------------------------------------ gate backward
 //
-// Three products around the gradient of the logits D [T][M + K] (columns: M local, then K group
-// logits): D itself from the probabilities, d_x = D W, and d_W = D^T X with the column sums of D.
-constexpr int kGbTok = 4;  // tokens (waves) per workgroup of the first launch
+// The gradient D [T][M + K] of the logits (columns: M local, then K group logits) from the probabilities, then
+// two products around it: d_x = D W and d_W = D^T X, with the column sums of D for the biases. Both have long
+// sides T and d and a short one R = M + K, and move X and d_x once: memory-bound, if the matrix cores are fast
+// enough. Float32 ones are not (4 T R d operations: 8192 x 2048, 72 rows: 31 us at their peak, against 13 us for the
+// 70 MB), so D is kept as three bfloat16 planes, D = hi + mid + lo up to 2^-24 |D|, whose products with bfloat16 X
+// and W are exact and summed in float32. d_x in bfloat16 takes two planes (2^-16 of each term, against 2^-8 for its
+// rounding). Float32 X and W are split the same way, and the pairs of planes below 2^-24 left out.
+// Contractions run down the rows of X, W and D: the gfx950 transposing LDS read gathers a lane's 4 values.
+constexpr int kGbWaves = 4;      // waves per workgroup, everywhere
+constexpr int kGbTokens = 8;     // tokens of a wave in the first launch
+constexpr int kDwStage = 64;     // tokens per LDS stage of d_W
+constexpr int kDwCols = 128;     // columns of a d_W workgroup
 
-inline int padded_rows(int R) { return (R + 15) / 16 * 16; }
+typedef short i16x4 __attribute__((ext_vector_type(4)));
 
-// One wave per token; lane l holds experts l, l + 64, ... D [T][ldd], zeros past M + K.
-__global__ __launch_bounds__(64 * kGbTok) void gate_logit_grad_kernel(GateBackwardArgs a, float* D, int ldd) {
-    constexpr int E = kMaxExperts / 64;
-    __shared__ float s_g[kGbTok][kMaxExperts], s_gd[kGbTok][kMaxExperts];
-    __shared__ float s_a[kGbTok][kMaxGroups], s_p[kGbTok][kMaxGroups];
-    __shared__ uint8_t s_grp[kMaxExperts];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int M = a.n_experts, K = a.n_groups, k = a.top_k;
-    for (int kk = threadIdx.x; kk < K; kk += 64 * kGbTok)
-        for (int i = a.goff[kk]; i < a.goff[kk + 1]; ++i) s_grp[i] = static_cast<uint8_t>(kk);
-    const int64_t t = static_cast<int64_t>(blockIdx.x) * kGbTok + wave;
-    const bool live = t < a.n_tokens && (!a.valid || a.valid[t]);
-    float* sg = s_g[wave];
-    float* sgd = s_gd[wave];
-    float g[E], dg[E];
-#pragma unroll
-    for (int j = 0; j < E; ++j) {
-        const int i = lane + 64 * j;
-        const bool in = live && i < M;
-        g[j] = in ? a.probs[t * M + i] : 0.f;
-        dg[j] = (in && a.d_balance ? a.d_balance[i] : 0.f) + (in && a.d_probs ? a.d_probs[t * M + i] : 0.f);
-        if (i < M) sg[i] = g[j];
-    }
-    __syncthreads();
-    if (a.d_topk_w && live) {  // uniform in the wave
-        int e = -1;
-        float dw = 0.f, gs = 0.f;
-        if (lane < k) {
-            e = a.topk_idx[t * k + lane];
-            if (e < 0 || e >= M) e = -1;
-            dw = a.d_topk_w[t * k + lane];
-            gs = e >= 0 ? sg[e] : 0.f;
-        }
-        if (a.renormalize) {
-            // w_j = g_j / S: dg_j = (dw_j - sum w dw) / S
-            float S = gs;
-#pragma unroll
-            for (int off = 1; off < 16; off <<= 1) S += __shfl_xor(S, off);
-            const float w = gs / S;
-            float m = lane < k ? w * dw : 0.f;
-#pragma unroll
-            for (int off = 1; off < 16; off <<= 1) m += __shfl_xor(m, off);
-            dw = (dw - m) / S;
-        }
-        for (int j = 0; j < k; ++j) {
-            const int ej = __shfl(e, j);
-            const float dj = __shfl(dw, j);
-#pragma unroll
-            for (int q = 0; q < E; ++q)
-                if (lane + 64 * q == ej) dg[q] += dj;
-        }
-    }
-#pragma unroll
-    for (int j = 0; j < E; ++j) {
-        const int i = lane + 64 * j;
-        if (i < M) sgd[i] = g[j] * dg[j];
-    }
-    __syncthreads();
-    float tot = 0.f;
-    for (int kk = lane; kk < K; kk += 64) {
-        float A = 0.f, P = 0.f;
-        for (int i = a.goff[kk]; i < a.goff[kk + 1]; ++i) {
-            A += sgd[i];
-            P += sg[i];
-        }
-        s_a[wave][kk] = A;
-        s_p[wave][kk] = P;
-        tot += A;
-    }
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) tot += __shfl_xor(tot, off);
-    __syncthreads();
-    if (t >= a.n_tokens) return;
-    float* row = D + t * ldd;
-#pragma unroll
-    for (int j = 0; j < E; ++j) {
-        const int i = lane + 64 * j;
-        if (i >= M) continue;
-        const int kk = s_grp[i];
-        const float P = s_p[wave][kk];
-        // a group without mass (no candidate, or underflow) has g = 0 throughout
-        row[i] = P > 0.f ? sgd[i] - g[j] / P * s_a[wave][kk] : sgd[i];
-    }
-    for (int i = M + lane; i < ldd; i += 64) row[i] = i < M + K ? s_a[wave][i - M] - s_p[wave][i - M] * tot : 0.f;
+// In each group of 16 lanes, lane i reads the 8 bytes at its address (elements S[i][0..3]) and receives
+// S[4 e + i / 4][i % 4] in element e: with lane i at row i / 4 and columns 4 (i % 4) .. + 3 of a row-major tile, the 4
+// rows of column i.
+__device__ __forceinline__ uint2 read_tr(const char* p) {
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                         (__attribute__((address_space(3))) i16x4*)(const_cast<char*>(p))));
+}
+__device__ __forceinline__ bf16x8 frag16(uint2 lo, uint2 hi) {
+    return __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
 }
 
-// value r of column c of the stacked gate weights (local rows, then group rows)
+// v = plane 0 + plane 1 + plane 2
+__device__ __forceinline__ void split3(float v, uint16_t (&pl)[3]) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        pl[i] = f32_to_bf16(v);
+        v -= bf16_to_f32(pl[i]);
+    }
+}
+
+template <typename T>
+constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1;  // of X and W
+template <typename T>
+constexpr int kDwRowBlocks = sizeof(T) == 4 ? 3 : 5;  // blocks of 16 logits of one d_W workgroup (registers)
+
+inline int logit_steps(int R) {  // contraction steps of 32 logits of d_x
+    const int n = (R + 31) / 32;
+    return n <= 1 ? 1 : n <= 3 ? 3 : n <= 5 ? 5 : 10;
+}
+
+// One wave per token, kGbTokens of them in turn; lane l holds experts l, l + 64, ... Writes the planes of D ([3][T][ldd],
+// zeros past M + K) and the workgroup's column sums.
+template <int E>
+__global__ __launch_bounds__(64 * kGbWaves) void gate_logit_grad_kernel(GateBackwardArgs a, uint16_t* D, int ldd,
+                                                                        float* bpart) {
+    constexpr int KQ = (kMaxGroups + 63) / 64;
+    __shared__ float s_g[kGbWaves][64 * E], s_gd[kGbWaves][64 * E];
+    __shared__ float s_a[kGbWaves][kMaxGroups], s_p[kGbWaves][kMaxGroups];
+    __shared__ uint8_t s_grp[64 * E];
+    __shared__ float s_sum[kGbWaves][64 * E + kMaxGroups];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int M = a.n_experts, K = a.n_groups, k = a.top_k;
+    for (int kk = threadIdx.x; kk < K; kk += 64 * kGbWaves)
+        for (int i = a.goff[kk]; i < a.goff[kk + 1]; ++i) s_grp[i] = static_cast<uint8_t>(kk);
+    int g0[KQ], g1[KQ];  // experts of the lane's groups
+#pragma unroll
+    for (int q = 0; q < KQ; ++q) {
+        const int kk = lane + 64 * q;
+        g0[q] = kk < K ? a.goff[kk] : 0;
+        g1[q] = kk < K ? a.goff[kk + 1] : 0;
+    }
+    float bal[E], suml[E], sumg[KQ];
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+        bal[j] = a.d_balance && lane + 64 * j < M ? a.d_balance[lane + 64 * j] : 0.f;
+        suml[j] = 0.f;
+    }
+#pragma unroll
+    for (int q = 0; q < KQ; ++q) sumg[q] = 0.f;
+    __syncthreads();
+    float* sg = s_g[wave];
+    float* sgd = s_gd[wave];
+    const int64_t plane = static_cast<int64_t>(a.n_tokens) * ldd;
+    const int64_t t0 = (static_cast<int64_t>(blockIdx.x) * kGbWaves + wave) * kGbTokens;
+    // Only this wave's LDS is shared below: its lanes run together, a wait for the LDS counter orders them.
+    auto settle = [&]() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
+    for (int u = 0; u < kGbTokens; ++u) {
+        const int64_t t = t0 + u;
+        if (t >= a.n_tokens) break;  // uniform in the wave
+        const bool live = !a.valid || a.valid[t];
+        float g[E], dg[E];
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const int i = lane + 64 * j;
+            const bool in = live && i < M;
+            g[j] = in ? a.probs[t * M + i] : 0.f;
+            dg[j] = (in ? bal[j] : 0.f) + (in && a.d_probs ? a.d_probs[t * M + i] : 0.f);
+            sg[i] = g[j];
+        }
+        int e = -1;
+        float dw = 0.f;
+        if (a.d_topk_w && live && lane < k) {
+            e = a.topk_idx[t * k + lane];
+            dw = a.d_topk_w[t * k + lane];
+        }
+        settle();
+        if (a.d_topk_w && live) {  // uniform in the wave
+            if (e < 0 || e >= M) e = -1;
+            const float gs = e >= 0 ? sg[e] : 0.f;
+            if (a.renormalize) {
+                // w_j = g_j / S: dg_j = (dw_j - sum w dw) / S
+                float S = gs;
+#pragma unroll
+                for (int off = 1; off < 16; off <<= 1) S += __shfl_xor(S, off);
+                float m = lane < k ? gs / S * dw : 0.f;
+#pragma unroll
+                for (int off = 1; off < 16; off <<= 1) m += __shfl_xor(m, off);
+                dw = (dw - m) / S;
+            }
+            for (int j = 0; j < k; ++j) {
+                const int ej = __builtin_amdgcn_readlane(e, j);
+                const float dj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(dw), j));
+#pragma unroll
+                for (int q = 0; q < E; ++q)
+                    if (lane + 64 * q == ej) dg[q] += dj;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < E; ++j) sgd[lane + 64 * j] = g[j] * dg[j];
+        settle();
+        float A[KQ], P[KQ], tot = 0.f;
+#pragma unroll
+        for (int q = 0; q < KQ; ++q) {
+            A[q] = P[q] = 0.f;
+            for (int i = g0[q]; i < g1[q]; ++i) {
+                A[q] += sgd[i];
+                P[q] += sg[i];
+            }
+            if (lane + 64 * q < K) {
+                s_a[wave][lane + 64 * q] = A[q];
+                s_p[wave][lane + 64 * q] = P[q];
+            }
+            tot += A[q];
+        }
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) tot += __shfl_xor(tot, off);
+        settle();
+        uint16_t* row = D + t * ldd;
+        auto put = [&](int c, float v) {
+            uint16_t pl[3];
+            split3(v, pl);
+#pragma unroll
+            for (int i = 0; i < 3; ++i) row[i * plane + c] = pl[i];
+        };
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const int i = lane + 64 * j;
+            if (i >= M) continue;
+            const int kk = s_grp[i];
+            const float Pk = s_p[wave][kk];
+            // a group without mass (no candidate, or underflow) has g = 0 throughout
+            const float v = Pk > 0.f ? sgd[i] - g[j] / Pk * s_a[wave][kk] : sgd[i];
+            suml[j] += v;
+            put(i, v);
+        }
+#pragma unroll
+        for (int q = 0; q < KQ; ++q) {
+            if (lane + 64 * q >= K) continue;
+            const float v = A[q] - P[q] * tot;
+            sumg[q] += v;
+            put(M + lane + 64 * q, v);
+        }
+        for (int i = M + K + lane; i < ldd; i += 64) put(i, 0.f);
+    }
+#pragma unroll
+    for (int j = 0; j < E; ++j)
+        if (lane + 64 * j < M) s_sum[wave][lane + 64 * j] = suml[j];
+#pragma unroll
+    for (int q = 0; q < KQ; ++q)
+        if (lane + 64 * q < K) s_sum[wave][M + lane + 64 * q] = sumg[q];
+    __syncthreads();
+    for (int r = threadIdx.x; r < M + K; r += 64 * kGbWaves) {
+        float v = s_sum[0][r];
+#pragma unroll
+        for (int w = 1; w < kGbWaves; ++w) v += s_sum[w][r];
+        bpart[static_cast<int64_t>(blockIdx.x) * (M + K) + r] = v;
+    }
+}
+
+// row r of the stacked gate weights (local rows, then group rows)
 template <typename T>
 __device__ __forceinline__ const T* gate_row(const GateBackwardArgs& a, int r) {
     return r < a.n_experts ? static_cast<const T*>(a.w_local) + static_cast<int64_t>(r) * a.d
                            : static_cast<const T*>(a.w_global) + static_cast<int64_t>(r - a.n_experts) * a.d;
 }
 
-// d_x [T][d] = D W: 16 tokens x 64 columns a wave, 4 waves side by side
-template <typename T>
-__global__ __launch_bounds__(256) void gate_dx_kernel(GateBackwardArgs a, const float* D, int ldd) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// 16 bytes as loaded (8 bfloat16 or 4 float32 values) into the planes of a staged tile, at byte offset off of a bfloat16
+// plane (float32 values take 8 bytes there)
+__device__ __forceinline__ void stage16(char* tile, int, int off, uint4 v, bf16_t) {
+    *reinterpret_cast<uint4*>(tile + off) = v;
+}
+__device__ __forceinline__ void stage16(char* tile, int plane_bytes, int off, uint4 v, float) {
+    const float f[4] = {__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w)};
+    uint16_t pl[4][3];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) split3(f[i], pl[i]);
+#pragma unroll
+    for (int p = 0; p < 3; ++p)
+        *reinterpret_cast<uint2*>(tile + p * plane_bytes + off) =
+            make_uint2(pl[0][p] | static_cast<uint32_t>(pl[1][p]) << 16, pl[2][p] | static_cast<uint32_t>(pl[3][p]) << 16);
+}
+
+// d_x [T][d] = D W. A workgroup holds the whole W [R][COLS] of its columns in LDS (the 32-byte chunk c of row r at c ^
+// (r % chunks), so that the 4 rows of a transposing read lie in different banks) and walks its tokens, 64 at a
+// time; the fragments of D come straight from memory (its lanes' 8 consecutive logits).
+template <typename T, int KS>
+__global__ __launch_bounds__(64 * kGbWaves) void gate_dx_kernel(GateBackwardArgs a, const uint16_t* D, int tokens) {
+    constexpr int PX = kPlanes<T>, PD = PX == 1 ? 2 : 3;
+    constexpr int COLS = PX == 1 ? 128 : 64, CB = COLS / 64;  // column blocks of 16 per wave
+    constexpr int ROWB = COLS * 2, CH = ROWB / 32, PLANE = KS * 32 * ROWB;
+    constexpr int LDD = KS * 32;
+    constexpr int EPC = Elem<T>::kPerChunk;
+    __shared__ __attribute__((aligned(16))) char w[PX * PLANE];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int l16 = lane & 15, lg = lane >> 4;
     const int R = a.n_experts + a.n_groups;
-    const int c0 = (blockIdx.y * 4 + wave) * 64;
-    if (c0 >= a.d) return;
-    const int64_t t = static_cast<int64_t>(blockIdx.x) * 16 + l16;
-    const float* drow = D + min(t, static_cast<int64_t>(a.n_tokens) - 1) * ldd;
-    f32x4 acc[4];
-#pragma unroll
-    for (int b = 0; b < 4; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int r0 = 0; r0 < R; r0 += 4) {
-        const int r = r0 + lg;
-        const float dv = drow[r];  // ldd is a multiple of 16: zeros past R
-        const T* w = gate_row<T>(a, min(r, R - 1)) + c0 + l16;
-#pragma unroll
-        for (int b = 0; b < 4; ++b)
-            acc[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(r < R ? Elem<T>::to_f32(w[16 * b]) : 0.f, dv, acc[b], 0, 0, 0);
+    const int c0 = blockIdx.x * COLS;
+    constexpr int PER_ROW = COLS / EPC;
+    for (int i = tid; i < KS * 32 * PER_ROW; i += 64 * kGbWaves) {
+        const int r = i / PER_ROW, e = (i % PER_ROW) * EPC;
+        const uint4 v = r < R ? ldg16(gate_row<T>(a, r) + c0 + e) : make_uint4(0, 0, 0, 0);
+        stage16(w, PLANE, r * ROWB + (((e / 16) ^ (r % CH)) * 32) + (e % 16) * 2, v, T{});
     }
-    if (t >= a.n_tokens) return;
-    T* out = static_cast<T*>(a.d_x) + t * a.d + c0 + 4 * lg;
+    __syncthreads();
+    const int64_t tb = static_cast<int64_t>(blockIdx.y) * tokens;
+    const int64_t te = min(tb + tokens, static_cast<int64_t>(a.n_tokens));
+    const int64_t plane = static_cast<int64_t>(a.n_tokens) * LDD;
+    for (int64_t t0 = tb; t0 < te; t0 += 64) {
+        f32x4 acc[CB][4];
 #pragma unroll
-    for (int b = 0; b < 4; ++b)
+        for (int c = 0; c < CB; ++c)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) out[16 * b + i] = Elem<T>::from_f32(acc[b][i]);
+            for (int m = 0; m < 4; ++m) acc[c][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const uint16_t* drow[4];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) drow[m] = D + min(t0 + m * 16 + l16, te - 1) * LDD + 8 * lg;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            uint4 dv[4][PD];
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+#pragma unroll
+                for (int p = 0; p < PD; ++p) dv[m][p] = ldg16(drow[m] + p * plane + ks * 32);
+            bf16x8 wv[CB][PX];
+#pragma unroll
+            for (int c = 0; c < CB; ++c)
+#pragma unroll
+                for (int p = 0; p < PX; ++p) {
+                    const int r = ks * 32 + 8 * lg + (l16 >> 2), chunk = wave * CB + c;
+                    const char* base = w + p * PLANE + (l16 & 3) * 8;
+                    wv[c][p] = frag16(read_tr(base + r * ROWB + (chunk ^ (r % CH)) * 32),
+                                      read_tr(base + (r + 4) * ROWB + (chunk ^ ((r + 4) % CH)) * 32));
+                }
+#pragma unroll
+            for (int c = 0; c < CB; ++c)
+#pragma unroll
+                for (int m = 0; m < 4; ++m)
+#pragma unroll
+                    for (int pd = PD - 1; pd >= 0; --pd)
+#pragma unroll
+                        for (int px = PX - 1; px >= 0; --px)
+                            if (pd + px <= 2)
+                                acc[c][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                    wv[c][px], __builtin_bit_cast(bf16x8, dv[m][pd]), acc[c][m], 0, 0, 0);
+        }
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            const int64_t t = t0 + m * 16 + l16;
+            if (t >= te) continue;
+            T* out = static_cast<T*>(a.d_x) + t * a.d + c0 + wave * CB * 16 + 4 * lg;
+#pragma unroll
+            for (int c = 0; c < CB; ++c) {
+                if constexpr (PX == 1) {
+                    uint2 o;
+                    o.x = static_cast<uint32_t>(f32_to_bf16(acc[c][m][0])) | static_cast<uint32_t>(f32_to_bf16(acc[c][m][1])) << 16;
+                    o.y = static_cast<uint32_t>(f32_to_bf16(acc[c][m][2])) | static_cast<uint32_t>(f32_to_bf16(acc[c][m][3])) << 16;
+                    *reinterpret_cast<uint2*>(out + 16 * c) = o;
+                } else {
+                    *reinterpret_cast<f32x4*>(out + 16 * c) = acc[c][m];
+                }
+            }
+        }
+    }
 }
 
-// part[chunk][r][c] = sum over the chunk's tokens of D[t][r] X[t][c]: 16 columns and every r a wave
+// part[chunk][r][c] = sum over the chunk's tokens of D[t][r] X[t][c], for NRB blocks of 16 logits from row group
+// blockIdx.z and 128 columns. Stages of 64 tokens: X as [token][128] (32-byte chunk c of row t at c ^ (t % 8)) and the
+// logits' columns of D as [token][16 NRB], per plane. Two waves take the column halves of the first 32 tokens of a
+// stage, two those of the others; their sums meet in LDS at the end. Padding tokens' rows of X count as zeros, whatever
+// they hold.
 template <typename T, int NRB>
-__global__ __launch_bounds__(256) void gate_dw_kernel(GateBackwardArgs a, const float* D, int ldd, int chunk, float* part) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+__global__ __launch_bounds__(64 * kGbWaves, 2) void gate_dw_kernel(GateBackwardArgs a, const uint16_t* D, int ldd,
+                                                                   int chunk, float* part) {
+    constexpr int PX = kPlanes<T>;
+    constexpr int EPC = Elem<T>::kPerChunk;
+    constexpr int XROW = kDwCols * 2, XPLANE = kDwStage * XROW;
+    constexpr int DROW = NRB * 32, DPLANE = kDwStage * DROW;
+    constexpr int XL = kDwStage * kDwCols / EPC / 256;            // 16-byte loads a thread
+    constexpr int DI = 3 * kDwStage * DROW / 16;                  // 16-byte pieces of a stage of D
+    constexpr int DL = (DI + 255) / 256;
+    constexpr int STAGE = PX * XPLANE + 3 * DPLANE;
+    constexpr int SUMS = 2 * NRB * 4 * 64 * 16;                   // two waves' sums
+    __shared__ __attribute__((aligned(16))) char lds[STAGE > SUMS ? STAGE : SUMS];
+    char* xs = lds;
+    char* ds = lds + PX * XPLANE;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int l16 = lane & 15, lg = lane >> 4;
-    const int c0 = (blockIdx.x * 4 + wave) * 16;
-    const int64_t t0 = static_cast<int64_t>(blockIdx.y) * chunk;
-    const int64_t t1 = min(t0 + chunk, static_cast<int64_t>(a.n_tokens));
-    const T* x = static_cast<const T*>(a.x) + c0 + l16;
-    f32x4 acc[NRB];
+    const int ch = wave & 1, th = wave >> 1;
+    const int c0 = blockIdx.x * kDwCols;
+    const int r0 = blockIdx.z * kDwRowBlocks<T> * 16;
+    const int64_t tb = static_cast<int64_t>(blockIdx.y) * chunk;
+    const int64_t te = min(tb + chunk, static_cast<int64_t>(a.n_tokens));
+    const int64_t plane = static_cast<int64_t>(a.n_tokens) * ldd;
+    uint4 xv[XL], dv[DL];
+    auto load = [&](int64_t t0) {
 #pragma unroll
-    for (int b = 0; b < NRB; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int64_t t = t0; t < t1; t += 4) {
-        const int64_t tt = t + lg;
-        const bool in = tt < t1;
-        const int64_t tc = in ? tt : t1 - 1;
-        const float xv = in ? Elem<T>::to_f32(x[tc * a.d]) : 0.f;
-        const float* drow = D + tc * ldd + l16;
+        for (int i = 0; i < XL; ++i) {
+            const int item = tid + 256 * i, row = item / (kDwCols / EPC), e = item % (kDwCols / EPC) * EPC;
+            const int64_t t = t0 + row;
+            const bool in = t < te && (!a.valid || a.valid[t]);
+            xv[i] = in ? ldg16(static_cast<const T*>(a.x) + t * a.d + c0 + e) : make_uint4(0, 0, 0, 0);
+        }
 #pragma unroll
-        for (int b = 0; b < NRB; ++b)
-            if (16 * b < ldd) acc[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(xv, in ? drow[16 * b] : 0.f, acc[b], 0, 0, 0);
-    }
-    float* out = part + static_cast<int64_t>(blockIdx.y) * ldd * a.d;
+        for (int i = 0; i < DL; ++i) {
+            const int item = tid + 256 * i, p = item / (DI / 3), q = item % (DI / 3);
+            const int64_t t = t0 + q / (DROW / 16);
+            const int c = r0 + q % (DROW / 16) * 8;
+            dv[i] = item < DI && t < te && c < ldd ? ldg16(D + p * plane + t * ldd + c) : make_uint4(0, 0, 0, 0);
+        }
+    };
+    f32x4 acc[NRB][4];
 #pragma unroll
     for (int b = 0; b < NRB; ++b)
-        if (16 * b < ldd) *reinterpret_cast<f32x4*>(out + static_cast<int64_t>(16 * b + l16) * a.d + c0 + 4 * lg) = acc[b];
-}
-
-// column sums of D over the chunk's tokens
-__global__ __launch_bounds__(320) void gate_db_kernel(const float* D, int ldd, int n_tokens, int chunk, float* part) {
-    const int r = threadIdx.x;
-    if (r >= ldd) return;
-    const int64_t t0 = static_cast<int64_t>(blockIdx.x) * chunk, t1 = min(t0 + chunk, static_cast<int64_t>(n_tokens));
-    float s = 0.f;
-#pragma unroll 8
-    for (int64_t t = t0; t < t1; ++t) s += D[t * ldd + r];
-    part[static_cast<int64_t>(blockIdx.x) * ldd + r] = s;
-}
-
-// the chunks' sums in order: rows r of 4 columns a thread, then the biases
-__global__ __launch_bounds__(256) void gate_dw_sum_kernel(GateBackwardArgs a, const float* part, const float* bpart,
-                                                          int ldd, int chunks) {
-    const int M = a.n_experts, R = M + a.n_groups;
-    const int64_t quads = static_cast<int64_t>(R) * (a.d / 4);
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    if (a.d_w_local && i < quads) {
-        const int r = static_cast<int>(i / (a.d / 4));
-        const int c = static_cast<int>(i % (a.d / 4)) * 4;
-        f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-        for (int j = 0; j < chunks; ++j)
-            s += *reinterpret_cast<const f32x4*>(part + (static_cast<int64_t>(j) * ldd + r) * a.d + c);
-        float* dst = r < M ? a.d_w_local + static_cast<int64_t>(r) * a.d : a.d_w_global + static_cast<int64_t>(r - M) * a.d;
-        *reinterpret_cast<f32x4*>(dst + c) = s;
-    }
-    if (blockIdx.x == 0)
-        for (int r = threadIdx.x; r < R; r += 256) {
-            double s = 0.0;
-            for (int j = 0; j < chunks; ++j) s += bpart[static_cast<int64_t>(j) * ldd + r];
-            float* dst = r < M ? a.d_b_local : a.d_b_global;
-            if (dst) dst[r < M ? r : r - M] = static_cast<float>(s);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) acc[b][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    load(tb);
+    for (int64_t t0 = tb; t0 < te; t0 += kDwStage) {
+        __syncthreads();  // every wave is done with the stage before
+#pragma unroll
+        for (int i = 0; i < XL; ++i) {
+            const int item = tid + 256 * i, row = item / (kDwCols / EPC), e = item % (kDwCols / EPC) * EPC;
+            stage16(xs, XPLANE, row * XROW + (((e / 16) ^ (row & 7)) * 32) + (e % 16) * 2, xv[i], T{});
         }
+#pragma unroll
+        for (int i = 0; i < DL; ++i) {
+            const int item = tid + 256 * i;
+            if (item < DI) *reinterpret_cast<uint4*>(ds + item * 16) = dv[i];
+        }
+        __syncthreads();
+        if (t0 + kDwStage < te) load(t0 + kDwStage);
+        const int row = th * 32 + 8 * lg + (l16 >> 2);
+        bf16x8 xf[4][PX];
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int p = 0; p < PX; ++p) {
+                const char* base = xs + p * XPLANE + (l16 & 3) * 8;
+                const int cc = ch * 4 + c;
+                xf[c][p] = frag16(read_tr(base + row * XROW + (cc ^ (row & 7)) * 32),
+                                  read_tr(base + (row + 4) * XROW + (cc ^ ((row + 4) & 7)) * 32));
+            }
+#pragma unroll
+        for (int b = 0; b < NRB; ++b) {
+            bf16x8 df[3];
+#pragma unroll
+            for (int p = 0; p < 3; ++p) {
+                const char* base = ds + p * DPLANE + b * 32 + (l16 & 3) * 8;
+                df[p] = frag16(read_tr(base + row * DROW), read_tr(base + (row + 4) * DROW));
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int pd = 2; pd >= 0; --pd)
+#pragma unroll
+                    for (int px = PX - 1; px >= 0; --px)
+                        if (pd + px <= 2)
+                            acc[b][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[c][px], df[pd], acc[b][c], 0, 0, 0);
+        }
+    }
+    __syncthreads();
+    f32x4* sums = reinterpret_cast<f32x4*>(lds) + ch * NRB * 4 * 64 + lane;
+    if (th == 1)
+#pragma unroll
+        for (int b = 0; b < NRB; ++b)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) sums[(b * 4 + c) * 64] = acc[b][c];
+    __syncthreads();
+    if (th == 1) return;
+    const int R = a.n_experts + a.n_groups;
+    float* out = part + static_cast<int64_t>(blockIdx.y) * R * a.d + c0 + ch * 64 + 4 * lg;
+#pragma unroll
+    for (int b = 0; b < NRB; ++b) {
+        const int r = r0 + b * 16 + l16;
+        if (r >= R) continue;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            *reinterpret_cast<f32x4*>(out + static_cast<int64_t>(r) * a.d + 16 * c) = acc[b][c] + sums[(b * 4 + c) * 64];
+    }
 }
 
-// Token chunks of d_W: about two workgroups a CU over the column tiles, 64 tokens or more each
-int dw_chunks(int n_tokens, int d) {
-    const int want = std::max(1, 512 / std::max(1, d / 64));
-    return std::max(1, std::min(want, (n_tokens + 63) / 64));
+// The chunks' sums in order: 4 columns of a row a thread; the first workgroups add the biases' partial sums instead, a
+// logit each (in float64, strided over the threads, then down a tree).
+__global__ __launch_bounds__(256) void gate_dw_sum_kernel(GateBackwardArgs a, const float* part, int chunks,
+                                                          const float* bpart, int bparts, int bias_groups) {
+    const int M = a.n_experts, R = M + a.n_groups;
+    if (static_cast<int>(blockIdx.x) < bias_groups) {
+        __shared__ double s[256];
+        const int r = blockIdx.x;
+        double v = 0.0;
+        for (int j = threadIdx.x; j < bparts; j += 256) v += bpart[static_cast<int64_t>(j) * R + r];
+        s[threadIdx.x] = v;
+        __syncthreads();
+        for (int h = 128; h > 0; h >>= 1) {
+            if (static_cast<int>(threadIdx.x) < h) s[threadIdx.x] += s[threadIdx.x + h];
+            __syncthreads();
+        }
+        float* dst = r < M ? a.d_b_local : a.d_b_global;
+        if (threadIdx.x == 0 && dst) dst[r < M ? r : r - M] = static_cast<float>(s[0]);
+        return;
+    }
+    const int64_t i = static_cast<int64_t>(blockIdx.x - bias_groups) * 256 + threadIdx.x;
+    if (i >= static_cast<int64_t>(R) * (a.d / 4)) return;
+    const int r = static_cast<int>(i / (a.d / 4));
+    const int c = static_cast<int>(i % (a.d / 4)) * 4;
+    f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int j = 0; j < chunks; ++j)
+        v += *reinterpret_cast<const f32x4*>(part + (static_cast<int64_t>(j) * R + r) * a.d + c);
+    float* dst = r < M ? a.d_w_local + static_cast<int64_t>(r) * a.d : a.d_w_global + static_cast<int64_t>(r - M) * a.d;
+    *reinterpret_cast<f32x4*>(dst + c) = v;
+}
+
+// Token chunks of d_W, whole stages each: about two workgroups a CU over the column tiles and row groups.
+int dw_chunk(int n_tokens, int d, int R, int row_blocks) {
+    const int tiles = (d / kDwCols) * ((R + 16 * row_blocks - 1) / (16 * row_blocks));
+    const int want = std::max(1, 512 / tiles);
+    const int per = (n_tokens + want - 1) / want;
+    return std::max(kDwStage, (per + kDwStage - 1) / kDwStage * kDwStage);
 }
 
 struct GateBackwardWs {
     size_t D, part, bpart, total;
+    int ldd, chunk, chunks, bparts;
 };
 
+template <typename T>
 GateBackwardWs gate_backward_ws(int n_tokens, int d, int R) {
-    const size_t ldd = padded_rows(R), ch = dw_chunks(n_tokens, d);
     auto up = [](size_t n) { return (n + 255) / 256 * 256; };
     GateBackwardWs w{};
+    w.ldd = 32 * logit_steps(R);
+    w.chunk = dw_chunk(n_tokens, d, R, kDwRowBlocks<T>);
+    w.chunks = (n_tokens + w.chunk - 1) / w.chunk;
+    w.bparts = (n_tokens + kGbWaves * kGbTokens - 1) / (kGbWaves * kGbTokens);
     size_t o = 0;
-    w.D = o; o += up(static_cast<size_t>(n_tokens) * ldd * 4);
-    w.part = o; o += up(ch * ldd * d * 4);
-    w.bpart = o; o += up(ch * ldd * 4);
+    w.D = o; o += up(static_cast<size_t>(n_tokens) * w.ldd * 2 * 3);
+    w.part = o; o += up(static_cast<size_t>(w.chunks) * R * d * 4);
+    w.bpart = o; o += up(static_cast<size_t>(w.bparts) * R * 4);
     w.total = o;
     return w;
 }
 
 template <typename T>
 hipError_t gate_backward(const GateBackwardArgs& a, hipStream_t s) {
-    const int R = a.n_experts + a.n_groups, ldd = padded_rows(R);
-    const GateBackwardWs w = gate_backward_ws(a.n_tokens, a.d, R);
+    const int R = a.n_experts + a.n_groups;
+    const GateBackwardWs w = gate_backward_ws<T>(a.n_tokens, a.d, R);
     char* base = static_cast<char*>(a.ws);
-    float* D = reinterpret_cast<float*>(base + w.D);
+    uint16_t* D = reinterpret_cast<uint16_t*>(base + w.D);
     float* part = reinterpret_cast<float*>(base + w.part);
     float* bpart = reinterpret_cast<float*>(base + w.bpart);
-    const int chunks = a.n_tokens ? dw_chunks(a.n_tokens, a.d) : 0;
-    const int chunk = chunks ? (a.n_tokens + chunks - 1) / chunks : 0;
+    const dim3 threads(64 * kGbWaves);
     hipError_t e = hipSuccess;
     if (a.n_tokens) {
         ProfileScope prof(kLogitGradName, s);
-        hipLaunchKernelGGL(gate_logit_grad_kernel, dim3((a.n_tokens + kGbTok - 1) / kGbTok), dim3(64 * kGbTok), 0, s, a, D, ldd);
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(w.bparts), threads, 0, s, a, D, w.ldd, bpart); };
+        if (a.n_experts <= 64) go(gate_logit_grad_kernel<1>);
+        else if (a.n_experts <= 128) go(gate_logit_grad_kernel<2>);
+        else go(gate_logit_grad_kernel<4>);
         e = hipGetLastError();
     }
     if (e == hipSuccess && a.n_tokens && a.d_x) {
         ProfileScope prof(kDxName, s);
-        hipLaunchKernelGGL(gate_dx_kernel<T>, dim3((a.n_tokens + 15) / 16, (a.d + 255) / 256), dim3(256), 0, s, a, D, ldd);
+        const int cols = kPlanes<T> == 1 ? 128 : 64;
+        // about four workgroups a CU, 64 tokens or more each
+        const int want = std::max(1, 1024 / (a.d / cols));
+        const int tokens = std::max(64, ((a.n_tokens + want - 1) / want + 63) / 64 * 64);
+        auto go = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3(a.d / cols, (a.n_tokens + tokens - 1) / tokens), threads, 0, s, a, D, tokens);
+        };
+        switch (logit_steps(R)) {
+            case 1: go(gate_dx_kernel<T, 1>); break;
+            case 3: go(gate_dx_kernel<T, 3>); break;
+            case 5: go(gate_dx_kernel<T, 5>); break;
+            default: go(gate_dx_kernel<T, 10>);
+        }
         e = hipGetLastError();
     }
     if (!a.d_w_local && !a.d_b_local && !a.d_b_global) return e;
     if (e == hipSuccess && a.n_tokens && a.d_w_local) {
         ProfileScope prof(kDwName, s);
+        const int nrb = (R + 15) / 16;
         auto go = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3(a.d / 64, chunks), dim3(256), 0, s, a, D, ldd, chunk, part);
+            hipLaunchKernelGGL(kernel, dim3(a.d / kDwCols, w.chunks, (nrb + kDwRowBlocks<T> - 1) / kDwRowBlocks<T>), threads, 0, s, a, D,
+                               w.ldd, w.chunk, part);
         };
-        const int nrb = ldd / 16;
         if (nrb <= 1) go(gate_dw_kernel<T, 1>);
         else if (nrb <= 2) go(gate_dw_kernel<T, 2>);
-        else if (nrb <= 5) go(gate_dw_kernel<T, 5>);
-        else if (nrb <= 10) go(gate_dw_kernel<T, 10>);
-        else go(gate_dw_kernel<T, 20>);
-        e = hipGetLastError();
-    }
-    if (e == hipSuccess && a.n_tokens) {
-        ProfileScope prof(kDbName, s);
-        hipLaunchKernelGGL(gate_db_kernel, dim3(chunks), dim3(320), 0, s, D, ldd, a.n_tokens, chunk, bpart);
+        else if (nrb <= 3) go(gate_dw_kernel<T, 3>);
+        else go(gate_dw_kernel<T, kDwRowBlocks<T>>);
         e = hipGetLastError();
     }
     if (e == hipSuccess) {
         ProfileScope prof(kDwSumName, s);
-        const int64_t quads = a.d_w_local ? static_cast<int64_t>(R) * (a.d / 4) : 1;
-        hipLaunchKernelGGL(gate_dw_sum_kernel, dim3(static_cast<unsigned>((quads + 255) / 256)), dim3(256), 0, s, a, part,
-                           bpart, ldd, chunks);
+        const int bias = a.d_b_local || a.d_b_global ? R : 0;
+        const int64_t quads = a.d_w_local ? static_cast<int64_t>(R) * (a.d / 4) : 0;
+        hipLaunchKernelGGL(gate_dw_sum_kernel, dim3(static_cast<unsigned>(bias + (quads + 255) / 256)), dim3(256), 0, s, a, part,
+                           w.chunks, bpart, w.bparts, bias);
         e = hipGetLastError();
     }
     return e;
@@ -443,8 +705,9 @@ hipError_t launch_balance(const BalanceArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
-size_t gate_backward_ws_bytes(DType, int n_tokens, int d, int n_experts, int n_groups) {
-    return gate_backward_ws(n_tokens, d, n_experts + n_groups).total;
+size_t gate_backward_ws_bytes(DType dt, int n_tokens, int d, int n_experts, int n_groups) {
+    const int R = n_experts + n_groups;
+    return dt == DType::BF16 ? gate_backward_ws<bf16_t>(n_tokens, d, R).total : gate_backward_ws<float>(n_tokens, d, R).total;
 }
 
 hipError_t launch_gate_backward(DType dt, const GateBackwardArgs& a, hipStream_t s) {

@@ -132,8 +132,8 @@ def test_gate_backward_matches_the_oracle(T, d, M, K, k, keep, uneven, renorm, t
     t = lambda a, ty=torch.float32: None if a is None else up(a, ty)
     call = lambda **kw: E.group_gate_backward(x, wg, wl, up(g), up(idx, torch.int32), t(dw), t(dp), t(db), t(valid, torch.bool),
                                               renormalize=renorm, group_sizes=sizes if uneven else None, **kw)
-    got = call()
-    dl, du, al, au = OO.gate_backward(g.astype(np.float64), idx, groups, renorm, dw, dp, db, valid)
+    got, g0 = call(), g.copy()
+    dl, du, al, au = OO.gate_backward(g0.astype(np.float64), idx, groups, renorm, dw, dp, db, valid)
     X, WG, WL = down(x), down(wg), down(wl)
     # a logit's gradient is a sum of up to M + k float32 terms of magnitudes al; products and sums over
     # the M + K logits, or the T tokens, add a rounding each; x, W and the probabilities are exact
@@ -141,6 +141,11 @@ def test_gate_backward_matches_the_oracle(T, d, M, K, k, keep, uneven, renorm, t
     el, eu = al * e0, au * e0
     if valid is not None:
         assert (down(got[0])[~valid] == 0).all()
+        # whatever a padding token holds, it reaches nothing
+        x[torch.from_numpy(~valid).to(DEV)] = float("nan")
+        g[~valid] = np.inf
+        assert all(torch.equal(u, v) for u, v in zip(got, call()))
+        x[torch.from_numpy(~valid).to(DEV)] = 0
     ref = dl @ WL + du @ WG
     _check("d_x", down(got[0]), ref, (el + al * (M + K) * 2.0 ** -24) @ np.abs(WL) + (eu + au * (M + K) * 2.0 ** -24) @ np.abs(WG)
            + np.abs(ref) * HALF[dtype] + 1e-37)
