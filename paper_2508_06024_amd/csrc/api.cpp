@@ -712,6 +712,7 @@ ec2moe_status ec2moe_group_gate_backward(const ec2moe_moe_desc* desc, const ec2m
             "top_groups %d of %d: the gradient needs every group's probabilities", top_groups, K);
     GateBackwardArgs a{};
     if (ec2moe_status st = group_offsets(desc, opts ? opts->group_sizes : nullptr, a.goff); st != EC2MOE_OK) return st;
+    a.group_size = sized ? 0 : M / K;
     const DType dt = static_cast<DType>(desc->dtype);
     const size_t need = gate_backward_ws_bytes(dt, T, desc->d_model, M, K);
     if (ec2moe_status st = check_ws(ws, ws_bytes, need); st != EC2MOE_OK) return st;

@@ -41,6 +41,7 @@ struct GateBackwardArgs {
     int n_tokens, d, n_experts, n_groups, top_k;
     bool renormalize;
     int32_t goff[161];       // group k = experts goff[k] .. goff[k + 1] - 1
+    int group_size;          // of equal groups; 0: see goff
     void* ws;                // gate_backward_ws_bytes()
 };
 size_t gate_backward_ws_bytes(DType dt, int n_tokens, int d, int n_experts, int n_groups);

@@ -163,7 +163,6 @@ __global__ __launch_bounds__(1024) void balance_finish_kernel(BalanceArgs a, int
 // rounding). Float32 X and W are split the same way, and the pairs of planes below 2^-24 left out.
 // Contractions run down the rows of X, W and D: the gfx950 transposing LDS read gathers a lane's 4 values.
 constexpr int kGbWaves = 4;      // waves per workgroup, everywhere
-constexpr int kGbTokens = 8;     // tokens of a wave in the first launch
 constexpr int kDwStage = 64;     // tokens per LDS stage of d_W
 constexpr int kDwCols = 128;     // columns of a d_W workgroup
 
@@ -199,43 +198,71 @@ inline int logit_steps(int R) {  // contraction steps of 32 logits of d_x
     return n <= 1 ? 1 : n <= 3 ? 3 : n <= 5 ? 5 : 10;
 }
 
-// One wave per token, kGbTokens of them in turn; lane l holds experts l, l + 64, ... Writes the planes of D ([3][T][ldd],
-// zeros past M + K) and the workgroup's column sums.
-template <int E>
-__global__ __launch_bounds__(64 * kGbWaves) void gate_logit_grad_kernel(GateBackwardArgs a, uint16_t* D, int ldd,
+// Sums over aligned runs of 2, 4, 8 or 16 lanes, which all lanes of the run receive (a lane's row is 16 lanes).
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float v) {
+    return v + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+// width: a power of two, 1 to 64, uniform
+__device__ __forceinline__ float run_sum(float v, int width) {
+    typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+    if (width > 1) v = dpp_add<0xB1>(v);   // lanes 1 0 3 2 of a quad
+    if (width > 2) v = dpp_add<0x4E>(v);   // lanes 2 3 0 1
+    if (width > 4) v = dpp_add<0x141>(v);  // mirrored within 8
+    if (width > 8) v = dpp_add<0x140>(v);  // mirrored within 16
+    if (width > 16) {
+        const u32x2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    if (width > 32) {
+        const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    return v;
+}
+
+// One wave per token, `tokens` of them in turn; lane l holds experts l, l + 64, ... Writes the planes of D ([3][T][ldd],
+// zeros past M + K) and the workgroup's column sums. RUNS: equal groups of a power of two up to 64 experts lie in
+// aligned runs of lanes, which sum over them in registers; else one lane sums a group from LDS.
+// Bound by the chain of a token's steps, so a wave takes few tokens (see the launch).
+template <int E, bool RUNS>
+__global__ __launch_bounds__(64 * kGbWaves) void gate_logit_grad_kernel(GateBackwardArgs a, uint16_t* D, int ldd, int tokens,
                                                                         float* bpart) {
-    constexpr int KQ = (kMaxGroups + 63) / 64;
-    __shared__ float s_g[kGbWaves][64 * E], s_gd[kGbWaves][64 * E];
-    __shared__ float s_a[kGbWaves][kMaxGroups], s_p[kGbWaves][kMaxGroups];
+    constexpr int KQ = RUNS ? 0 : (kMaxGroups + 63) / 64;
+    __shared__ float s_g[kGbWaves][64 * E], s_gd[RUNS ? 1 : kGbWaves][64 * E];
+    __shared__ float s_a[RUNS ? 1 : kGbWaves][kMaxGroups], s_p[RUNS ? 1 : kGbWaves][kMaxGroups];
     __shared__ uint8_t s_grp[64 * E];
     __shared__ float s_sum[kGbWaves][64 * E + kMaxGroups];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int M = a.n_experts, K = a.n_groups, k = a.top_k;
-    for (int kk = threadIdx.x; kk < K; kk += 64 * kGbWaves)
-        for (int i = a.goff[kk]; i < a.goff[kk + 1]; ++i) s_grp[i] = static_cast<uint8_t>(kk);
-    int g0[KQ], g1[KQ];  // experts of the lane's groups
+    int g0[KQ + 1], g1[KQ + 1];  // experts of the lane's groups
+    if constexpr (!RUNS) {
+        for (int kk = threadIdx.x; kk < K; kk += 64 * kGbWaves)
+            for (int i = a.goff[kk]; i < a.goff[kk + 1]; ++i) s_grp[i] = static_cast<uint8_t>(kk);
 #pragma unroll
-    for (int q = 0; q < KQ; ++q) {
-        const int kk = lane + 64 * q;
-        g0[q] = kk < K ? a.goff[kk] : 0;
-        g1[q] = kk < K ? a.goff[kk + 1] : 0;
+        for (int q = 0; q < KQ; ++q) {
+            const int kk = lane + 64 * q;
+            g0[q] = kk < K ? a.goff[kk] : 0;
+            g1[q] = kk < K ? a.goff[kk + 1] : 0;
+        }
+        __syncthreads();
     }
-    float bal[E], suml[E], sumg[KQ];
+    const int mk = a.group_size;
+    float bal[E], suml[E], sumg[RUNS ? E : KQ];
 #pragma unroll
     for (int j = 0; j < E; ++j) {
         bal[j] = a.d_balance && lane + 64 * j < M ? a.d_balance[lane + 64 * j] : 0.f;
         suml[j] = 0.f;
     }
 #pragma unroll
-    for (int q = 0; q < KQ; ++q) sumg[q] = 0.f;
-    __syncthreads();
+    for (int q = 0; q < (RUNS ? E : KQ); ++q) sumg[q] = 0.f;
     float* sg = s_g[wave];
-    float* sgd = s_gd[wave];
+    float* sgd = s_gd[RUNS ? 0 : wave];
     const int64_t plane = static_cast<int64_t>(a.n_tokens) * ldd;
-    const int64_t t0 = (static_cast<int64_t>(blockIdx.x) * kGbWaves + wave) * kGbTokens;
+    const int64_t t0 = (static_cast<int64_t>(blockIdx.x) * kGbWaves + wave) * tokens;
     // Only this wave's LDS is shared below: its lanes run together, a wait for the LDS counter orders them.
     auto settle = [&]() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
-    for (int u = 0; u < kGbTokens; ++u) {
+    for (int u = 0; u < tokens; ++u) {
         const int64_t t = t0 + u;
         if (t >= a.n_tokens) break;  // uniform in the wave
         const bool live = !a.valid || a.valid[t];
@@ -260,12 +287,8 @@ __global__ __launch_bounds__(64 * kGbWaves) void gate_logit_grad_kernel(GateBack
             const float gs = e >= 0 ? sg[e] : 0.f;
             if (a.renormalize) {
                 // w_j = g_j / S: dg_j = (dw_j - sum w dw) / S
-                float S = gs;
-#pragma unroll
-                for (int off = 1; off < 16; off <<= 1) S += __shfl_xor(S, off);
-                float m = lane < k ? gs / S * dw : 0.f;
-#pragma unroll
-                for (int off = 1; off < 16; off <<= 1) m += __shfl_xor(m, off);
+                const float S = run_sum(gs, 16);
+                const float m = run_sum(lane < k ? gs / S * dw : 0.f, 16);
                 dw = (dw - m) / S;
             }
             for (int j = 0; j < k; ++j) {
@@ -276,26 +299,6 @@ __global__ __launch_bounds__(64 * kGbWaves) void gate_logit_grad_kernel(GateBack
                     if (lane + 64 * q == ej) dg[q] += dj;
             }
         }
-#pragma unroll
-        for (int j = 0; j < E; ++j) sgd[lane + 64 * j] = g[j] * dg[j];
-        settle();
-        float A[KQ], P[KQ], tot = 0.f;
-#pragma unroll
-        for (int q = 0; q < KQ; ++q) {
-            A[q] = P[q] = 0.f;
-            for (int i = g0[q]; i < g1[q]; ++i) {
-                A[q] += sgd[i];
-                P[q] += sg[i];
-            }
-            if (lane + 64 * q < K) {
-                s_a[wave][lane + 64 * q] = A[q];
-                s_p[wave][lane + 64 * q] = P[q];
-            }
-            tot += A[q];
-        }
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) tot += __shfl_xor(tot, off);
-        settle();
         uint16_t* row = D + t * ldd;
         auto put = [&](int c, float v) {
             uint16_t pl[3];
@@ -303,29 +306,75 @@ __global__ __launch_bounds__(64 * kGbWaves) void gate_logit_grad_kernel(GateBack
 #pragma unroll
             for (int i = 0; i < 3; ++i) row[i * plane + c] = pl[i];
         };
+        // a group without mass (no candidate, or underflow) has g = 0 throughout
+        auto local = [&](float gd, float gj, float A, float P) { return P > 0.f ? gd - gj / P * A : gd; };
+        if constexpr (RUNS) {
+            float gd[E], tot = 0.f;
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-            const int i = lane + 64 * j;
-            if (i >= M) continue;
-            const int kk = s_grp[i];
-            const float Pk = s_p[wave][kk];
-            // a group without mass (no candidate, or underflow) has g = 0 throughout
-            const float v = Pk > 0.f ? sgd[i] - g[j] / Pk * s_a[wave][kk] : sgd[i];
-            suml[j] += v;
-            put(i, v);
-        }
+            for (int j = 0; j < E; ++j) {
+                gd[j] = g[j] * dg[j];
+                tot += gd[j];
+            }
+            tot = run_sum(tot, 64);
 #pragma unroll
-        for (int q = 0; q < KQ; ++q) {
-            if (lane + 64 * q >= K) continue;
-            const float v = A[q] - P[q] * tot;
-            sumg[q] += v;
-            put(M + lane + 64 * q, v);
+            for (int j = 0; j < E; ++j) {
+                const int i = lane + 64 * j;
+                const float A = run_sum(gd[j], mk), P = run_sum(g[j], mk);
+                if (i >= M) continue;
+                const float v = local(gd[j], g[j], A, P);
+                suml[j] += v;
+                put(i, v);
+                if ((i & (mk - 1)) == 0) {  // the group's first lane: its group logit
+                    const float w = A - P * tot;
+                    sumg[j] += w;
+                    put(M + i / mk, w);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < E; ++j) sgd[lane + 64 * j] = g[j] * dg[j];
+            settle();
+            float A[KQ + 1], P[KQ + 1], tot = 0.f;
+#pragma unroll
+            for (int q = 0; q < KQ; ++q) {
+                A[q] = P[q] = 0.f;
+                for (int i = g0[q]; i < g1[q]; ++i) {
+                    A[q] += sgd[i];
+                    P[q] += sg[i];
+                }
+                if (lane + 64 * q < K) {
+                    s_a[wave][lane + 64 * q] = A[q];
+                    s_p[wave][lane + 64 * q] = P[q];
+                }
+                tot += A[q];
+            }
+            tot = run_sum(tot, 64);
+            settle();
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                const int i = lane + 64 * j;
+                if (i >= M) continue;
+                const int kk = s_grp[i];
+                const float v = local(sgd[i], g[j], s_a[wave][kk], s_p[wave][kk]);
+                suml[j] += v;
+                put(i, v);
+            }
+#pragma unroll
+            for (int q = 0; q < KQ; ++q) {
+                if (lane + 64 * q >= K) continue;
+                const float v = A[q] - P[q] * tot;
+                sumg[q] += v;
+                put(M + lane + 64 * q, v);
+            }
         }
         for (int i = M + K + lane; i < ldd; i += 64) put(i, 0.f);
     }
 #pragma unroll
-    for (int j = 0; j < E; ++j)
-        if (lane + 64 * j < M) s_sum[wave][lane + 64 * j] = suml[j];
+    for (int j = 0; j < E; ++j) {
+        const int i = lane + 64 * j;
+        if (i < M) s_sum[wave][i] = suml[j];
+        if (RUNS && i < M && (i & (mk - 1)) == 0) s_sum[wave][M + i / mk] = sumg[RUNS ? j : 0];
+    }
 #pragma unroll
     for (int q = 0; q < KQ; ++q)
         if (lane + 64 * q < K) s_sum[wave][M + lane + 64 * q] = sumg[q];
@@ -361,21 +410,49 @@ __device__ __forceinline__ void stage16(char* tile, int plane_bytes, int off, ui
             make_uint2(pl[0][p] | static_cast<uint32_t>(pl[1][p]) << 16, pl[2][p] | static_cast<uint32_t>(pl[3][p]) << 16);
 }
 
+// Column tile and token chunk of a workgroup: the column tiles of a chunk run on one XCD (workgroups go round-robin over
+// the eight), so that its rows of D are fetched into that XCD's L2 once. Chunks at or past `chunks` have no work.
+__device__ __forceinline__ int2 col_chunk(int cols, int chunks) {
+    const int b = blockIdx.x, j = b / 8;
+    return make_int2(j % cols, j / cols * 8 + b % 8);
+}
+inline unsigned col_chunk_grid(int cols, int chunks) { return static_cast<unsigned>(cols) * ((chunks + 7) / 8) * 8; }
+
 // d_x [T][d] = D W. A workgroup holds the whole W [R][COLS] of its columns in LDS (the 32-byte chunk c of row r at c ^
 // (r % chunks), so that the 4 rows of a transposing read lie in different banks) and walks its tokens, 64 at a
 // time; the fragments of D come straight from memory (its lanes' 8 consecutive logits).
 template <typename T, int KS>
-__global__ __launch_bounds__(64 * kGbWaves) void gate_dx_kernel(GateBackwardArgs a, const uint16_t* D, int tokens) {
+__global__ __launch_bounds__(64 * kGbWaves) void gate_dx_kernel(GateBackwardArgs a, const uint16_t* D, int tokens, int chunks) {
     constexpr int PX = kPlanes<T>, PD = PX == 1 ? 2 : 3;
     constexpr int COLS = PX == 1 ? 128 : 64, CB = COLS / 64;  // column blocks of 16 per wave
     constexpr int ROWB = COLS * 2, CH = ROWB / 32, PLANE = KS * 32 * ROWB;
     constexpr int LDD = KS * 32;
+    constexpr int MB = 2;                // token blocks of a step
+    constexpr int NK = KS <= 3 ? KS : 1;  // contraction steps loaded together, one set ahead
     constexpr int EPC = Elem<T>::kPerChunk;
     __shared__ __attribute__((aligned(16))) char w[PX * PLANE];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int l16 = lane & 15, lg = lane >> 4;
     const int R = a.n_experts + a.n_groups;
-    const int c0 = blockIdx.x * COLS;
+    const int2 at = col_chunk(a.d / COLS, chunks);
+    if (at.y >= chunks) return;
+    const int c0 = at.x * COLS;
+    const int64_t tb = static_cast<int64_t>(at.y) * tokens;
+    const int64_t te = min(tb + tokens, static_cast<int64_t>(a.n_tokens));
+    const int64_t plane = static_cast<int64_t>(a.n_tokens) * LDD;
+    // the fragments of D of NK steps of the 16 MB tokens from t0
+    auto load = [&](int64_t t0, int ks0, uint4 (&dv)[NK][MB][PD]) {
+#pragma unroll
+        for (int m = 0; m < MB; ++m) {
+            const uint16_t* drow = D + min(t0 + m * 16 + l16, te - 1) * LDD + 8 * lg;
+#pragma unroll
+            for (int ks = 0; ks < NK; ++ks)
+#pragma unroll
+                for (int p = 0; p < PD; ++p) dv[ks][m][p] = ldg16(drow + p * plane + (ks0 + ks) * 32);
+        }
+    };
+    uint4 dv[NK][MB][PD], nx[NK][MB][PD];
+    load(tb, 0, nx);
     constexpr int PER_ROW = COLS / EPC;
     for (int i = tid; i < KS * 32 * PER_ROW; i += 64 * kGbWaves) {
         const int r = i / PER_ROW, e = (i % PER_ROW) * EPC;
@@ -383,49 +460,45 @@ __global__ __launch_bounds__(64 * kGbWaves) void gate_dx_kernel(GateBackwardArgs
         stage16(w, PLANE, r * ROWB + (((e / 16) ^ (r % CH)) * 32) + (e % 16) * 2, v, T{});
     }
     __syncthreads();
-    const int64_t tb = static_cast<int64_t>(blockIdx.y) * tokens;
-    const int64_t te = min(tb + tokens, static_cast<int64_t>(a.n_tokens));
-    const int64_t plane = static_cast<int64_t>(a.n_tokens) * LDD;
-    for (int64_t t0 = tb; t0 < te; t0 += 64) {
-        f32x4 acc[CB][4];
+    for (int64_t t0 = tb; t0 < te; t0 += 16 * MB) {
+        f32x4 acc[CB][MB];
 #pragma unroll
         for (int c = 0; c < CB; ++c)
 #pragma unroll
-            for (int m = 0; m < 4; ++m) acc[c][m] = f32x4{0.f, 0.f, 0.f, 0.f};
-        const uint16_t* drow[4];
+            for (int m = 0; m < MB; ++m) acc[c][m] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int m = 0; m < 4; ++m) drow[m] = D + min(t0 + m * 16 + l16, te - 1) * LDD + 8 * lg;
+        for (int ks0 = 0; ks0 < KS; ks0 += NK) {
+            __builtin_memcpy(dv, nx, sizeof dv);
+            if (ks0 + NK < KS) load(t0, ks0 + NK, nx);
+            else if (t0 + 16 * MB < te) load(t0 + 16 * MB, 0, nx);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            uint4 dv[4][PD];
+            for (int kk = 0; kk < NK; ++kk) {
+                const int ks = ks0 + kk;
+                bf16x8 wv[CB][PX];
 #pragma unroll
-            for (int m = 0; m < 4; ++m)
+                for (int c = 0; c < CB; ++c)
 #pragma unroll
-                for (int p = 0; p < PD; ++p) dv[m][p] = ldg16(drow[m] + p * plane + ks * 32);
-            bf16x8 wv[CB][PX];
+                    for (int p = 0; p < PX; ++p) {
+                        const int r = ks * 32 + 8 * lg + (l16 >> 2), chunk = wave * CB + c;
+                        const char* base = w + p * PLANE + (l16 & 3) * 8;
+                        wv[c][p] = frag16(read_tr(base + r * ROWB + (chunk ^ (r % CH)) * 32),
+                                          read_tr(base + (r + 4) * ROWB + (chunk ^ ((r + 4) % CH)) * 32));
+                    }
 #pragma unroll
-            for (int c = 0; c < CB; ++c)
+                for (int c = 0; c < CB; ++c)
 #pragma unroll
-                for (int p = 0; p < PX; ++p) {
-                    const int r = ks * 32 + 8 * lg + (l16 >> 2), chunk = wave * CB + c;
-                    const char* base = w + p * PLANE + (l16 & 3) * 8;
-                    wv[c][p] = frag16(read_tr(base + r * ROWB + (chunk ^ (r % CH)) * 32),
-                                      read_tr(base + (r + 4) * ROWB + (chunk ^ ((r + 4) % CH)) * 32));
-                }
+                    for (int m = 0; m < MB; ++m)
 #pragma unroll
-            for (int c = 0; c < CB; ++c)
+                        for (int pd = PD - 1; pd >= 0; --pd)
 #pragma unroll
-                for (int m = 0; m < 4; ++m)
-#pragma unroll
-                    for (int pd = PD - 1; pd >= 0; --pd)
-#pragma unroll
-                        for (int px = PX - 1; px >= 0; --px)
-                            if (pd + px <= 2)
-                                acc[c][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                                    wv[c][px], __builtin_bit_cast(bf16x8, dv[m][pd]), acc[c][m], 0, 0, 0);
+                            for (int px = PX - 1; px >= 0; --px)
+                                if (pd + px <= 2)
+                                    acc[c][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                        wv[c][px], __builtin_bit_cast(bf16x8, dv[kk][m][pd]), acc[c][m], 0, 0, 0);
+            }
         }
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
+        for (int m = 0; m < MB; ++m) {
             const int64_t t = t0 + m * 16 + l16;
             if (t >= te) continue;
             T* out = static_cast<T*>(a.d_x) + t * a.d + c0 + wave * CB * 16 + 4 * lg;
@@ -445,13 +518,13 @@ __global__ __launch_bounds__(64 * kGbWaves) void gate_dx_kernel(GateBackwardArgs
 }
 
 // part[chunk][r][c] = sum over the chunk's tokens of D[t][r] X[t][c], for NRB blocks of 16 logits from row group
-// blockIdx.z and 128 columns. Stages of 64 tokens: X as [token][128] (32-byte chunk c of row t at c ^ (t % 8)) and the
+// blockIdx.y and 128 columns. Stages of 64 tokens: X as [token][128] (32-byte chunk c of row t at c ^ (t % 8)) and the
 // logits' columns of D as [token][16 NRB], per plane. Two waves take the column halves of the first 32 tokens of a
 // stage, two those of the others; their sums meet in LDS at the end. Padding tokens' rows of X count as zeros, whatever
 // they hold.
 template <typename T, int NRB>
 __global__ __launch_bounds__(64 * kGbWaves, 2) void gate_dw_kernel(GateBackwardArgs a, const uint16_t* D, int ldd,
-                                                                   int chunk, float* part) {
+                                                                   int chunk, int chunks, float* part) {
     constexpr int PX = kPlanes<T>;
     constexpr int EPC = Elem<T>::kPerChunk;
     constexpr int XROW = kDwCols * 2, XPLANE = kDwStage * XROW;
@@ -467,9 +540,11 @@ __global__ __launch_bounds__(64 * kGbWaves, 2) void gate_dw_kernel(GateBackwardA
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int l16 = lane & 15, lg = lane >> 4;
     const int ch = wave & 1, th = wave >> 1;
-    const int c0 = blockIdx.x * kDwCols;
-    const int r0 = blockIdx.z * kDwRowBlocks<T> * 16;
-    const int64_t tb = static_cast<int64_t>(blockIdx.y) * chunk;
+    const int2 at = col_chunk(a.d / kDwCols, chunks);
+    if (at.y >= chunks) return;
+    const int c0 = at.x * kDwCols;
+    const int r0 = blockIdx.y * kDwRowBlocks<T> * 16;
+    const int64_t tb = static_cast<int64_t>(at.y) * chunk;
     const int64_t te = min(tb + chunk, static_cast<int64_t>(a.n_tokens));
     const int64_t plane = static_cast<int64_t>(a.n_tokens) * ldd;
     uint4 xv[XL], dv[DL];
@@ -548,7 +623,7 @@ __global__ __launch_bounds__(64 * kGbWaves, 2) void gate_dw_kernel(GateBackwardA
     __syncthreads();
     if (th == 1) return;
     const int R = a.n_experts + a.n_groups;
-    float* out = part + static_cast<int64_t>(blockIdx.y) * R * a.d + c0 + ch * 64 + 4 * lg;
+    float* out = part + static_cast<int64_t>(at.y) * R * a.d + c0 + ch * 64 + 4 * lg;
 #pragma unroll
     for (int b = 0; b < NRB; ++b) {
         const int r = r0 + b * 16 + l16;
@@ -601,7 +676,7 @@ int dw_chunk(int n_tokens, int d, int R, int row_blocks) {
 
 struct GateBackwardWs {
     size_t D, part, bpart, total;
-    int ldd, chunk, chunks, bparts;
+    int ldd, chunk, chunks, tokens, bparts;
 };
 
 template <typename T>
@@ -611,7 +686,9 @@ GateBackwardWs gate_backward_ws(int n_tokens, int d, int R) {
     w.ldd = 32 * logit_steps(R);
     w.chunk = dw_chunk(n_tokens, d, R, kDwRowBlocks<T>);
     w.chunks = (n_tokens + w.chunk - 1) / w.chunk;
-    w.bparts = (n_tokens + kGbWaves * kGbTokens - 1) / (kGbWaves * kGbTokens);
+    // a token a wave up to four workgroups a CU; more only lengthen the list of the biases' partial sums
+    w.tokens = std::max(1, std::min(16, n_tokens / (1024 * kGbWaves)));
+    w.bparts = (n_tokens + kGbWaves * w.tokens - 1) / (kGbWaves * w.tokens);
     size_t o = 0;
     w.D = o; o += up(static_cast<size_t>(n_tokens) * w.ldd * 2 * 3);
     w.part = o; o += up(static_cast<size_t>(w.chunks) * R * d * 4);
@@ -632,10 +709,12 @@ hipError_t gate_backward(const GateBackwardArgs& a, hipStream_t s) {
     hipError_t e = hipSuccess;
     if (a.n_tokens) {
         ProfileScope prof(kLogitGradName, s);
-        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(w.bparts), threads, 0, s, a, D, w.ldd, bpart); };
-        if (a.n_experts <= 64) go(gate_logit_grad_kernel<1>);
-        else if (a.n_experts <= 128) go(gate_logit_grad_kernel<2>);
-        else go(gate_logit_grad_kernel<4>);
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(w.bparts), threads, 0, s, a, D, w.ldd, w.tokens, bpart); };
+        const int mk = a.group_size;
+        const bool runs = mk > 0 && mk <= 64 && (mk & (mk - 1)) == 0;
+        if (a.n_experts <= 64) runs ? go(gate_logit_grad_kernel<1, true>) : go(gate_logit_grad_kernel<1, false>);
+        else if (a.n_experts <= 128) runs ? go(gate_logit_grad_kernel<2, true>) : go(gate_logit_grad_kernel<2, false>);
+        else runs ? go(gate_logit_grad_kernel<4, true>) : go(gate_logit_grad_kernel<4, false>);
         e = hipGetLastError();
     }
     if (e == hipSuccess && a.n_tokens && a.d_x) {
@@ -645,7 +724,8 @@ hipError_t gate_backward(const GateBackwardArgs& a, hipStream_t s) {
         const int want = std::max(1, 1024 / (a.d / cols));
         const int tokens = std::max(64, ((a.n_tokens + want - 1) / want + 63) / 64 * 64);
         auto go = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3(a.d / cols, (a.n_tokens + tokens - 1) / tokens), threads, 0, s, a, D, tokens);
+            const int chunks = (a.n_tokens + tokens - 1) / tokens;
+            hipLaunchKernelGGL(kernel, dim3(col_chunk_grid(a.d / cols, chunks)), threads, 0, s, a, D, tokens, chunks);
         };
         switch (logit_steps(R)) {
             case 1: go(gate_dx_kernel<T, 1>); break;
@@ -660,8 +740,8 @@ hipError_t gate_backward(const GateBackwardArgs& a, hipStream_t s) {
         ProfileScope prof(kDwName, s);
         const int nrb = (R + 15) / 16;
         auto go = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3(a.d / kDwCols, w.chunks, (nrb + kDwRowBlocks<T> - 1) / kDwRowBlocks<T>), threads, 0, s, a, D,
-                               w.ldd, w.chunk, part);
+            hipLaunchKernelGGL(kernel, dim3(col_chunk_grid(a.d / kDwCols, w.chunks), (nrb + kDwRowBlocks<T> - 1) / kDwRowBlocks<T>),
+                               threads, 0, s, a, D, w.ldd, w.chunk, w.chunks, part);
         };
         if (nrb <= 1) go(gate_dw_kernel<T, 1>);
         else if (nrb <= 2) go(gate_dw_kernel<T, 2>);
