@@ -19,10 +19,13 @@ constexpr const char *kBalanceName = "balance_loss", *kBalanceFinishName = "bala
 // ------------------------------------------------------------------ load balance loss
 //
 // Column sums of probs over the valid tokens and a histogram of the selected experts, by chunks of
-// tokens (a workgroup each); a second launch adds the chunks in order. With one chunk the first
-// launch finishes by itself. Integer counts are added with LDS atomics: their order changes nothing.
-constexpr int kBalThreads = 256;
+// tokens (a workgroup each); a second launch adds the chunks in order, a workgroup per 32 experts, and the last of its
+// workgroups to arrive adds their shares of the loss in order. With one chunk the first launch finishes by itself.
+// Integer counts are added with LDS atomics: their order changes nothing. Memory-bound (probs once) for long batches;
+// short ones are two launches.
+constexpr int kBalThreads = 512;
 constexpr int kBalMaxChunks = 512;
+constexpr int kBalCols = 32;  // experts of a workgroup of the second launch
 
 int balance_chunks(int n_tokens, int n_experts) {
     const int64_t values = static_cast<int64_t>(n_tokens) * n_experts;
@@ -30,34 +33,28 @@ int balance_chunks(int n_tokens, int n_experts) {
 }
 
 struct BalancePart {
-    float* p;    // [chunks][M]
-    int32_t* c;  // [chunks][M]
-    int32_t* n;  // [chunks] valid tokens
+    double* loss;    // [kMaxExperts / kBalCols] shares of the second launch's workgroups
+    uint32_t* done;  // its workgroups that have finished (cleared by the first launch)
+    float* p;        // [chunks][M]
+    int32_t* c;      // [chunks][M]
+    int32_t* n;      // [chunks] valid tokens
 };
 
 __host__ __device__ inline BalancePart balance_part(void* ws, int chunks, int M) {
-    float* p = static_cast<float*>(ws);
+    double* loss = static_cast<double*>(ws);
+    uint32_t* done = reinterpret_cast<uint32_t*>(loss + kMaxExperts / kBalCols);
+    float* p = reinterpret_cast<float*>(done + 2);
     int32_t* c = reinterpret_cast<int32_t*>(p + static_cast<size_t>(chunks) * M);
-    return {p, c, c + static_cast<size_t>(chunks) * M};
+    return {loss, done, p, c, c + static_cast<size_t>(chunks) * M};
 }
 
-// Thread e < M of a workgroup holds expert e's sum of probabilities and count, n the valid tokens: writes
-// the outputs. sm: kMaxExperts doubles.
-__device__ __forceinline__ void balance_outputs(const BalanceArgs& a, int e, double p, int c, int n, double* sm) {
-    const int M = a.n_experts;
+// Expert e of the sum of probabilities p and count c over n valid tokens: writes its outputs, returns its share of the loss.
+__device__ __forceinline__ double balance_expert(const BalanceArgs& a, int e, double p, int c, int n) {
     double d = 0.0;
-    if (e < M) {
-        if (n > 0) d = static_cast<double>(a.coef) * M * c / (static_cast<double>(a.top_k) * n * n);
-        if (a.counts) a.counts[e] = c;
-        if (a.d_probs) a.d_probs[e] = static_cast<float>(d);
-        sm[e] = n > 0 ? d * p : 0.0;
-    }
-    __syncthreads();
-    if (e == 0) {
-        double loss = 0.0;
-        for (int i = 0; i < M; ++i) loss += sm[i];
-        a.loss[0] = static_cast<float>(loss);
-    }
+    if (n > 0) d = static_cast<double>(a.coef) * a.n_experts * c / (static_cast<double>(a.top_k) * n * n);
+    if (a.counts) a.counts[e] = c;
+    if (a.d_probs) a.d_probs[e] = static_cast<float>(d);
+    return n > 0 ? d * p : 0.0;
 }
 
 // V: consecutive experts a thread loads together
@@ -67,11 +64,14 @@ __global__ __launch_bounds__(kBalThreads) void balance_kernel(BalanceArgs a, int
     __shared__ int s_cnt[kMaxExperts];
     __shared__ int s_n;
     __shared__ double s_loss[kMaxExperts];
-    const int tid = threadIdx.x, M = a.n_experts;
+    const int tid = threadIdx.x, M = a.n_experts, k = a.top_k;
     const int L = (M + V - 1) / V;         // threads per row
     const int RP = kBalThreads / L;        // rows per pass
     const int64_t t0 = static_cast<int64_t>(blockIdx.x) * chunk;
-    const int64_t t1 = min(t0 + chunk, static_cast<int64_t>(a.n_tokens));
+    const int nt = static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(chunk), a.n_tokens - t0)));
+    const float* probs = a.probs + t0 * M;
+    const int32_t* idx = a.topk_idx + t0 * k;
+    const uint8_t* valid = a.valid ? a.valid + t0 : nullptr;
     for (int i = tid; i < kMaxExperts; i += kBalThreads) s_cnt[i] = 0;
     if (tid == 0) s_n = 0;
     __syncthreads();
@@ -80,25 +80,35 @@ __global__ __launch_bounds__(kBalThreads) void balance_kernel(BalanceArgs a, int
 #pragma unroll
     for (int v = 0; v < V; ++v) sum[v] = 0.f;
     if (rs < RP) {
+        // (a token that does not count adds zero, not its value times zero)
 #pragma unroll 8
-        for (int64_t t = t0 + rs; t < t1; t += RP) {
-            const bool ok = !a.valid || a.valid[t];
+        for (int t = rs; t < nt; t += RP) {
+            const bool ok = !valid || valid[t];
             if constexpr (V == 4) {
-                const f32x4 v = *reinterpret_cast<const f32x4*>(a.probs + t * M + c);
+                const f32x4 v = *reinterpret_cast<const f32x4*>(probs + static_cast<int64_t>(t) * M + c);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) sum[i] += ok ? v[i] : 0.f;
             } else {
-                sum[0] += ok ? a.probs[t * M + c] : 0.f;
+                const float v = probs[static_cast<int64_t>(t) * M + c];
+                sum[0] += ok ? v : 0.f;
             }
         }
     }
-    for (int64_t i = t0 * a.top_k + tid; i < t1 * a.top_k; i += kBalThreads) {
-        const int e = a.topk_idx[i];
-        if ((!a.valid || a.valid[i / a.top_k]) && e >= 0 && e < M) atomicAdd(&s_cnt[e], 1);
+    // a thread keeps its slot of the token: 256 / k tokens a pass
+    const int tp = kBalThreads / k, slot = tid % k;
+#pragma unroll 4
+    for (int t = tid / k; t < nt; t += tp) {
+        if (tid / k >= tp) break;
+        const int e = idx[static_cast<int64_t>(t) * k + slot];
+        if ((!valid || valid[t]) && e >= 0 && e < M) atomicAdd(&s_cnt[e], 1);
     }
     int n = 0;
-    for (int64_t t = t0 + tid; t < t1; t += kBalThreads) n += !a.valid || a.valid[t] ? 1 : 0;
-    if (n) atomicAdd(&s_n, n);
+    if (valid) {
+        for (int t = tid; t < nt; t += kBalThreads) n += valid[t] ? 1 : 0;
+        if (n) atomicAdd(&s_n, n);
+    } else if (tid == 0) {
+        s_n = nt;
+    }
     if (rs < RP)
 #pragma unroll
         for (int v = 0; v < V; ++v) s_sum[rs * L * V + c + v] = sum[v];
@@ -107,7 +117,13 @@ __global__ __launch_bounds__(kBalThreads) void balance_kernel(BalanceArgs a, int
     if (tid < M)
         for (int r = 0; r < RP; ++r) p += s_sum[r * L * V + tid];
     if (gridDim.x == 1) {
-        balance_outputs(a, tid, p, tid < M ? s_cnt[tid] : 0, s_n, s_loss);
+        if (tid < M) s_loss[tid] = balance_expert(a, tid, p, s_cnt[tid], s_n);
+        __syncthreads();
+        if (tid == 0) {
+            double loss = 0.0;
+            for (int i = 0; i < M; ++i) loss += s_loss[i];
+            a.loss[0] = static_cast<float>(loss);
+        }
         return;
     }
     const BalancePart part = balance_part(a.ws, gridDim.x, M);
@@ -115,41 +131,56 @@ __global__ __launch_bounds__(kBalThreads) void balance_kernel(BalanceArgs a, int
         part.p[static_cast<int64_t>(blockIdx.x) * M + tid] = p;
         part.c[static_cast<int64_t>(blockIdx.x) * M + tid] = s_cnt[tid];
     }
-    if (tid == 0) part.n[blockIdx.x] = s_n;
+    if (tid == 0) {
+        part.n[blockIdx.x] = s_n;
+        if (blockIdx.x == 0) part.done[0] = 0;
+    }
 }
 
 __global__ __launch_bounds__(1024) void balance_finish_kernel(BalanceArgs a, int chunks) {
-    __shared__ double s_p[1024];
-    __shared__ int s_c[1024];
+    constexpr int SLOTS = 1024 / kBalCols;
+    __shared__ double s_p[SLOTS][kBalCols];
+    __shared__ int s_c[SLOTS][kBalCols];
     __shared__ int s_n;
-    __shared__ double s_loss[kMaxExperts];
+    __shared__ double s_loss[kBalCols];
     const int tid = threadIdx.x, M = a.n_experts;
-    const int slots = 1024 / M;
-    const int e = tid % M, slot = tid / M;
+    const int col = tid % kBalCols, slot = tid / kBalCols, e = blockIdx.x * kBalCols + col;
     const BalancePart part = balance_part(a.ws, chunks, M);
     if (tid == 0) s_n = 0;
     __syncthreads();
     double p = 0.0;
     int c = 0, n = 0;
-    if (slot < slots)
+    if (e < M)
 #pragma unroll 8
-        for (int j = slot; j < chunks; j += slots) {
+        for (int j = slot; j < chunks; j += SLOTS) {
             p += part.p[static_cast<int64_t>(j) * M + e];
             c += part.c[static_cast<int64_t>(j) * M + e];
         }
     for (int j = tid; j < chunks; j += 1024) n += part.n[j];
     if (n) atomicAdd(&s_n, n);
-    s_p[tid] = p;
-    s_c[tid] = c;
+    s_p[slot][col] = p;
+    s_c[slot][col] = c;
     __syncthreads();
-    p = 0.0;
-    c = 0;
-    if (tid < M)
-        for (int j = 0; j < slots; ++j) {
-            p += s_p[j * M + tid];
-            c += s_c[j * M + tid];
+    if (slot == 0) {
+        for (int j = 1; j < SLOTS; ++j) {
+            p += s_p[j][col];
+            c += s_c[j][col];
         }
-    balance_outputs(a, tid, p, c, s_n, s_loss);
+        s_loss[col] = e < M ? balance_expert(a, e, p, c, s_n) : 0.0;
+    }
+    __syncthreads();
+    if (tid != 0) return;
+    double loss = 0.0;
+    for (int i = 0; i < kBalCols; ++i) loss += s_loss[i];
+    if (gridDim.x > 1) {
+        __hip_atomic_store(part.loss + blockIdx.x, loss, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const uint32_t before = __hip_atomic_fetch_add(part.done, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+        if (before + 1 != gridDim.x) return;
+        loss = 0.0;
+        for (unsigned i = 0; i < gridDim.x; ++i)
+            loss += __hip_atomic_load(part.loss + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    a.loss[0] = static_cast<float>(loss);
 }
 
 // ------------------------------------------------------------------ gate backward
@@ -419,18 +450,22 @@ __device__ __forceinline__ int2 col_chunk(int cols, int chunks) {
 inline unsigned col_chunk_grid(int cols, int chunks) { return static_cast<unsigned>(cols) * ((chunks + 7) / 8) * 8; }
 
 // d_x [T][d] = D W. A workgroup holds the whole W [R][COLS] of its columns in LDS (the 32-byte chunk c of row r at c ^
-// (r % chunks), so that the 4 rows of a transposing read lie in different banks) and walks its tokens, 64 at a
-// time; the fragments of D come straight from memory (its lanes' 8 consecutive logits).
+// (r % chunks), so that the 4 rows of a transposing read lie in different banks); its waves walk the tokens, 32 each at
+// a time, over all the columns. The fragments of D come straight from memory (a lane's 8 consecutive logits), a set
+// ahead. Finished rows are turned in LDS (each wave its own 4 KB) so that a store covers whole 256-byte rows: stores of
+// 8 bytes a lane, 32 bytes of a row, took 26 us in place of 18 (8192 tokens of 2048, 72 logits).
 template <typename T, int KS>
 __global__ __launch_bounds__(64 * kGbWaves) void gate_dx_kernel(GateBackwardArgs a, const uint16_t* D, int tokens, int chunks) {
     constexpr int PX = kPlanes<T>, PD = PX == 1 ? 2 : 3;
-    constexpr int COLS = PX == 1 ? 128 : 64, CB = COLS / 64;  // column blocks of 16 per wave
+    constexpr int COLS = PX == 1 ? 128 : 64, CB = COLS / 16;  // column blocks of 16
     constexpr int ROWB = COLS * 2, CH = ROWB / 32, PLANE = KS * 32 * ROWB;
     constexpr int LDD = KS * 32;
-    constexpr int MB = 2;                // token blocks of a step
+    constexpr int MB = 2;                 // token blocks of a step
     constexpr int NK = KS <= 3 ? KS : 1;  // contraction steps loaded together, one set ahead
     constexpr int EPC = Elem<T>::kPerChunk;
+    constexpr int STEP = 16 * MB * kGbWaves;  // tokens of the workgroup's step
     __shared__ __attribute__((aligned(16))) char w[PX * PLANE];
+    __shared__ __attribute__((aligned(16))) char turn[kGbWaves][16 * 256];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int l16 = lane & 15, lg = lane >> 4;
     const int R = a.n_experts + a.n_groups;
@@ -452,7 +487,8 @@ __global__ __launch_bounds__(64 * kGbWaves) void gate_dx_kernel(GateBackwardArgs
         }
     };
     uint4 dv[NK][MB][PD], nx[NK][MB][PD];
-    load(tb, 0, nx);
+    int64_t t0 = tb + wave * 16 * MB;
+    load(t0, 0, nx);
     constexpr int PER_ROW = COLS / EPC;
     for (int i = tid; i < KS * 32 * PER_ROW; i += 64 * kGbWaves) {
         const int r = i / PER_ROW, e = (i % PER_ROW) * EPC;
@@ -460,7 +496,7 @@ __global__ __launch_bounds__(64 * kGbWaves) void gate_dx_kernel(GateBackwardArgs
         stage16(w, PLANE, r * ROWB + (((e / 16) ^ (r % CH)) * 32) + (e % 16) * 2, v, T{});
     }
     __syncthreads();
-    for (int64_t t0 = tb; t0 < te; t0 += 16 * MB) {
+    for (; t0 < te; t0 += STEP) {
         f32x4 acc[CB][MB];
 #pragma unroll
         for (int c = 0; c < CB; ++c)
@@ -470,22 +506,19 @@ __global__ __launch_bounds__(64 * kGbWaves) void gate_dx_kernel(GateBackwardArgs
         for (int ks0 = 0; ks0 < KS; ks0 += NK) {
             __builtin_memcpy(dv, nx, sizeof dv);
             if (ks0 + NK < KS) load(t0, ks0 + NK, nx);
-            else if (t0 + 16 * MB < te) load(t0 + 16 * MB, 0, nx);
+            else if (t0 + STEP < te) load(t0 + STEP, 0, nx);
 #pragma unroll
             for (int kk = 0; kk < NK; ++kk) {
-                const int ks = ks0 + kk;
-                bf16x8 wv[CB][PX];
+                const int r = (ks0 + kk) * 32 + 8 * lg + (l16 >> 2);
 #pragma unroll
-                for (int c = 0; c < CB; ++c)
+                for (int c = 0; c < CB; ++c) {
+                    bf16x8 wv[PX];
 #pragma unroll
                     for (int p = 0; p < PX; ++p) {
-                        const int r = ks * 32 + 8 * lg + (l16 >> 2), chunk = wave * CB + c;
                         const char* base = w + p * PLANE + (l16 & 3) * 8;
-                        wv[c][p] = frag16(read_tr(base + r * ROWB + (chunk ^ (r % CH)) * 32),
-                                          read_tr(base + (r + 4) * ROWB + (chunk ^ ((r + 4) % CH)) * 32));
+                        wv[p] = frag16(read_tr(base + r * ROWB + (c ^ (r % CH)) * 32),
+                                       read_tr(base + (r + 4) * ROWB + (c ^ ((r + 4) % CH)) * 32));
                     }
-#pragma unroll
-                for (int c = 0; c < CB; ++c)
 #pragma unroll
                     for (int m = 0; m < MB; ++m)
 #pragma unroll
@@ -494,25 +527,34 @@ __global__ __launch_bounds__(64 * kGbWaves) void gate_dx_kernel(GateBackwardArgs
                             for (int px = PX - 1; px >= 0; --px)
                                 if (pd + px <= 2)
                                     acc[c][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                                        wv[c][px], __builtin_bit_cast(bf16x8, dv[kk][m][pd]), acc[c][m], 0, 0, 0);
+                                        wv[px], __builtin_bit_cast(bf16x8, dv[kk][m][pd]), acc[c][m], 0, 0, 0);
+                }
             }
         }
+        // 16 rows of 256 bytes: the 16-byte chunk x of row r at x ^ r
 #pragma unroll
         for (int m = 0; m < MB; ++m) {
-            const int64_t t = t0 + m * 16 + l16;
-            if (t >= te) continue;
-            T* out = static_cast<T*>(a.d_x) + t * a.d + c0 + wave * CB * 16 + 4 * lg;
+            char* row = turn[wave] + l16 * 256;
 #pragma unroll
             for (int c = 0; c < CB; ++c) {
                 if constexpr (PX == 1) {
                     uint2 o;
                     o.x = static_cast<uint32_t>(f32_to_bf16(acc[c][m][0])) | static_cast<uint32_t>(f32_to_bf16(acc[c][m][1])) << 16;
                     o.y = static_cast<uint32_t>(f32_to_bf16(acc[c][m][2])) | static_cast<uint32_t>(f32_to_bf16(acc[c][m][3])) << 16;
-                    *reinterpret_cast<uint2*>(out + 16 * c) = o;
+                    *reinterpret_cast<uint2*>(row + (((2 * c + (lg >> 1)) ^ l16) * 16) + (lg & 1) * 8) = o;
                 } else {
-                    *reinterpret_cast<f32x4*>(out + 16 * c) = acc[c][m];
+                    *reinterpret_cast<f32x4*>(row + (((4 * c + lg) ^ l16) * 16)) = acc[c][m];
                 }
             }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the wave's own rows
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = 4 * i + lg;
+                const int64_t t = t0 + m * 16 + r;
+                const uint4 v = *reinterpret_cast<const uint4*>(turn[wave] + r * 256 + ((l16 ^ r) * 16));
+                if (t < te) stg16(static_cast<T*>(a.d_x) + t * a.d + c0 + l16 * EPC, v);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read before the next rows land
         }
     }
 }
@@ -666,10 +708,12 @@ __global__ __launch_bounds__(256) void gate_dw_sum_kernel(GateBackwardArgs a, co
     *reinterpret_cast<f32x4*>(dst + c) = v;
 }
 
-// Token chunks of d_W, whole stages each: about two workgroups a CU over the column tiles and row groups.
+// Token chunks of d_W, whole stages each: as many workgroups over the column tiles and row groups as the CUs hold at once
+// (4, 3 or 2 a CU by their registers).
 int dw_chunk(int n_tokens, int d, int R, int row_blocks) {
-    const int tiles = (d / kDwCols) * ((R + 16 * row_blocks - 1) / (16 * row_blocks));
-    const int want = std::max(1, 512 / tiles);
+    const int nrb = (R + 15) / 16;
+    const int tiles = (d / kDwCols) * ((nrb + row_blocks - 1) / row_blocks);
+    const int want = std::max(1, 256 * (nrb == 1 ? 4 : nrb == 2 ? 3 : 2) / tiles);
     const int per = (n_tokens + want - 1) / want;
     return std::max(kDwStage, (per + kDwStage - 1) / kDwStage * kDwStage);
 }
@@ -720,9 +764,9 @@ hipError_t gate_backward(const GateBackwardArgs& a, hipStream_t s) {
     if (e == hipSuccess && a.n_tokens && a.d_x) {
         ProfileScope prof(kDxName, s);
         const int cols = kPlanes<T> == 1 ? 128 : 64;
-        // about four workgroups a CU, 64 tokens or more each
-        const int want = std::max(1, 1024 / (a.d / cols));
-        const int tokens = std::max(64, ((a.n_tokens + want - 1) / want + 63) / 64 * 64);
+        // about three workgroups a CU, whole steps of 128 tokens each
+        const int want = std::max(1, 768 / (a.d / cols));
+        const int step = 32 * kGbWaves, tokens = std::max(step, ((a.n_tokens + want - 1) / want + step - 1) / step * step);
         auto go = [&](auto kernel) {
             const int chunks = (a.n_tokens + tokens - 1) / tokens;
             hipLaunchKernelGGL(kernel, dim3(col_chunk_grid(a.d / cols, chunks)), threads, 0, s, a, D, tokens, chunks);
@@ -764,7 +808,7 @@ hipError_t gate_backward(const GateBackwardArgs& a, hipStream_t s) {
 
 size_t balance_ws_bytes(int n_tokens, int n_experts) {
     const size_t chunks = balance_chunks(n_tokens, n_experts);
-    return chunks == 1 ? 0 : chunks * (2 * static_cast<size_t>(n_experts) + 1) * 4;
+    return chunks == 1 ? 0 : (kMaxExperts / kBalCols) * 8 + 8 + chunks * (2 * static_cast<size_t>(n_experts) + 1) * 4;
 }
 
 hipError_t launch_balance(const BalanceArgs& a, hipStream_t s) {
@@ -781,7 +825,7 @@ hipError_t launch_balance(const BalanceArgs& a, hipStream_t s) {
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || chunks == 1) return e;
     ProfileScope prof(kBalanceFinishName, s);
-    hipLaunchKernelGGL(balance_finish_kernel, dim3(1), dim3(1024), 0, s, a, chunks);
+    hipLaunchKernelGGL(balance_finish_kernel, dim3((a.n_experts + kBalCols - 1) / kBalCols), dim3(1024), 0, s, a, chunks);
     return hipGetLastError();
 }
 
