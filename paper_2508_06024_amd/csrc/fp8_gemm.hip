@@ -50,7 +50,7 @@ __device__ __forceinline__ void store_run(TO* dst, f32x4 v, int left, bool whole
 // A tile of 16 MT token rows and 16 NT weight rows (SwiGLU: NT gate and NT up blocks) by WAVES waves that
 // take every WAVES-th block of K, fragments straight from memory; their sums meet in LDS and are added
 // in wave order.
-template <typename TO, int MT, int NT, int WAVES, Epilogue EPI>
+template <typename TO, int MT, int NT, int WAVES, int U, Epilogue EPI>
 __global__ __launch_bounds__(64 * WAVES) void fp8_skinny_kernel(Fp8GemmArgs p) {
     constexpr bool SWIGLU = EPI == Epilogue::SwiGLU;
     constexpr int NB = SWIGLU ? 2 * NT : NT;  // weight blocks
@@ -90,32 +90,41 @@ __global__ __launch_bounds__(64 * WAVES) void fp8_skinny_kernel(Fp8GemmArgs p) {
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) acc[nb][mt] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    for (int kb = wave; kb < nkb; kb += WAVES) {
-        const int64_t off = static_cast<int64_t>(kb) * kFp8Block;
-        i32x8 fw[NB], ft[MT];
-        float sw[NB], st[MT];
+    // U blocks of K in flight; those past the end repeat the last one and count zero
+    for (int kb0 = wave; kb0 < nkb; kb0 += WAVES * U) {
+        i32x8 fw[U][NB], ft[U][MT];
+        float sw[U][NB], st[U][MT];
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            fw[nb] = frag8(ldg16(wrow[nb] + off), ldg16(wrow[nb] + off + 64));
-            sw[nb] = wscale[nb][kb];
-        }
+        for (int u = 0; u < U; ++u) {
+            const int kb = min(kb0 + u * WAVES, nkb - 1);
+            const int64_t off = static_cast<int64_t>(kb) * kFp8Block;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            ft[mt] = frag8(ldg16(trow[mt] + off), ldg16(trow[mt] + off + 64));
-            st[mt] = tscale[mt][kb];
-        }
-        Wide wt[MT];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) wt[mt] = widen(ft[mt]);
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            const Wide ww = widen(fw[nb]);
+            for (int nb = 0; nb < NB; ++nb) {
+                fw[u][nb] = frag8(ldg16_nt(wrow[nb] + off), ldg16_nt(wrow[nb] + off + 64));
+                sw[u][nb] = wscale[nb][kb];
+            }
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
-                const f32x4 part = mfma_wide(ww, wt[mt]);
-                const float s = sw[nb] * st[mt];
+                ft[u][mt] = frag8(ldg16(trow[mt] + off), ldg16(trow[mt] + off + 64));
+                st[u][mt] = tscale[mt][kb];
+            }
+        }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[nb][mt][i] = fmaf(part[i], s, acc[nb][mt][i]);
+        for (int u = 0; u < U; ++u) {
+            if (kb0 + u * WAVES >= nkb) break;  // uniform
+            Wide wt[MT];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) wt[mt] = widen(ft[u][mt]);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                const Wide ww = widen(fw[u][nb]);
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    const f32x4 part = mfma_wide(ww, wt[mt]);
+                    const float s = sw[u][nb] * st[u][mt];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[nb][mt][i] = fmaf(part[i], s, acc[nb][mt][i]);
+                }
             }
         }
     }
@@ -161,8 +170,8 @@ __device__ __forceinline__ int weight_row(const Fp8GemmArgs& p, int nt, int n) {
 // Tiles of TM x 128 over the whole K: slabs of one block of 128 (128-byte pieces of each row) go through
 // a ring of RING LDS stages filled by buffer_load ... lds, RING - 1 of them in flight behind counted waits
 // and one barrier per slab. Four waves of TM x 32. Chunk c of staged row R sits at c ^ ((R >> 1) & 7).
-// EXACT: products through bfloat16.
-template <typename TO, int TM, int RING, Epilogue EPI, bool EXACT>
+// STREAM: the weights pass the caches by (each is read once).
+template <typename TO, int TM, int RING, Epilogue EPI, bool STREAM>
 __global__ __launch_bounds__(256, 2) void fp8_ring_kernel(Fp8GemmArgs p) {
     constexpr bool SWIGLU = EPI == Epilogue::SwiGLU;
     constexpr int TN = 128;
@@ -210,7 +219,8 @@ __global__ __launch_bounds__(256, 2) void fp8_ring_kernel(Fp8GemmArgs p) {
         for (int j = 0; j < NLD; ++j) {
             const bool tok = 8 * (NLD * wave + j) < TM;  // uniform
             lds_void* dst = reinterpret_cast<lds_void*>(reinterpret_cast<uintptr_t>(slot + 1024 * (NLD * wave + j)));
-            raw_buffer_load_lds(tok ? rtok : rw, dst, 16, static_cast<int>(voff[j]), st * kFp8Block, 0, 0);
+            if (tok) raw_buffer_load_lds(rtok, dst, 16, static_cast<int>(voff[j]), st * kFp8Block, 0, 0);
+            else raw_buffer_load_lds(rw, dst, 16, static_cast<int>(voff[j]), st * kFp8Block, 0, STREAM ? 2 : 0);
         }
     };
 
@@ -277,21 +287,14 @@ __global__ __launch_bounds__(256, 2) void fp8_ring_kernel(Fp8GemmArgs p) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[ni][mi][i] = fmaf(part[i], s[ni][mi], acc[ni][mi][i]);
         };
-        if constexpr (EXACT) {
-            Wide ww[NI];
+        Wide ww[NI];
 #pragma unroll
-            for (int ni = 0; ni < NI; ++ni) ww[ni] = widen(fw[ni]);
+        for (int ni = 0; ni < NI; ++ni) ww[ni] = widen(fw[ni]);
 #pragma unroll
-            for (int mi = 0; mi < MI; ++mi) {
-                const Wide wt = widen(ft[mi]);
+        for (int mi = 0; mi < MI; ++mi) {
+            const Wide wt = widen(ft[mi]);
 #pragma unroll
-                for (int ni = 0; ni < NI; ++ni) add(ni, mi, mfma_wide(ww[ni], wt));
-            }
-        } else {
-#pragma unroll
-            for (int mi = 0; mi < MI; ++mi)
-#pragma unroll
-                for (int ni = 0; ni < NI; ++ni) add(ni, mi, mfma8(fw[ni], ft[mi]));
+            for (int ni = 0; ni < NI; ++ni) add(ni, mi, mfma_wide(ww[ni], wt));
         }
     };
     load_scales(0);
@@ -742,18 +745,18 @@ unsigned tile_grid(const Fp8GemmArgs& a, int tm, int tn) {
     return static_cast<unsigned>((max_tiles(a, tm, tn) + kXcds - 1) / kXcds * kXcds);
 }
 
-template <typename TO, int MT, int NT, int WAVES, Epilogue EPI>
+template <typename TO, int MT, int NT, int WAVES, int U, Epilogue EPI>
 hipError_t run_skinny(const Fp8GemmArgs& a, hipStream_t s) {
     ProfileScope prof(a.name, s);
-    hipLaunchKernelGGL((fp8_skinny_kernel<TO, MT, NT, WAVES, EPI>), dim3(tile_grid(a, 16 * MT, 16 * NT)), dim3(64 * WAVES), 0,
+    hipLaunchKernelGGL((fp8_skinny_kernel<TO, MT, NT, WAVES, U, EPI>), dim3(tile_grid(a, 16 * MT, 16 * NT)), dim3(64 * WAVES), 0,
                        s, a);
     return hipGetLastError();
 }
 
-template <typename TO, int TM, int RING, Epilogue EPI, bool EXACT>
+template <typename TO, int TM, int RING, Epilogue EPI, bool STREAM>
 hipError_t run_ring(const Fp8GemmArgs& a, hipStream_t s) {
     ProfileScope prof(a.name, s);
-    hipLaunchKernelGGL((fp8_ring_kernel<TO, TM, RING, EPI, EXACT>), dim3(tile_grid(a, TM, EPI == Epilogue::SwiGLU ? 64 : 128)),
+    hipLaunchKernelGGL((fp8_ring_kernel<TO, TM, RING, EPI, STREAM>), dim3(tile_grid(a, TM, EPI == Epilogue::SwiGLU ? 64 : 128)),
                        dim3(256), 0, s, a);
     return hipGetLastError();
 }
@@ -776,11 +779,12 @@ bool use_pp(const Fp8GemmArgs& a) {
     return offsets32(a) && avg_rows(a) >= 256 && a.K >= 2 * kFp8Block;
 }
 
-template <typename TO, Epilogue EPI, bool EXACT>
+template <typename TO, Epilogue EPI>
 hipError_t dispatch_small(const Fp8GemmArgs& a, hipStream_t s) {
-    constexpr int NT = EPI == Epilogue::SwiGLU ? 2 : 4;
-    if (avg_rows(a) < 16 || !offsets32(a)) return run_skinny<TO, 1, NT, 4, EPI>(a, s);
-    return run_ring<TO, 64, 3, EPI, EXACT>(a, s);
+    const int tn = EPI == Epilogue::SwiGLU ? 64 : 128;
+    if (!offsets32(a) || (avg_rows(a) < 32 && max_tiles(a, 32, tn) < 512)) return run_skinny<TO, 1, 1, 8, 4, EPI>(a, s);
+    if (avg_rows(a) < 16) return run_ring<TO, 32, 4, EPI, true>(a, s);
+    return run_ring<TO, 64, 3, EPI, false>(a, s);
 }
 
 }  // namespace
@@ -797,9 +801,9 @@ bool fp8_gemm_fits(int64_t rows, int n_groups, int64_t n) {
 
 hipError_t launch_fp8_gemm(DType out_type, const Fp8GemmArgs& a, hipStream_t s) {
     if (a.rows == 0) return hipSuccess;
-    if (out_type == DType::F32) return dispatch_small<float, Epilogue::Store, true>(a, s);
+    if (out_type == DType::F32) return dispatch_small<float, Epilogue::Store>(a, s);
     if (use_pp(a) && a.N % 8 == 0) return run_pp<Epilogue::Store>(a, s);
-    return dispatch_small<bf16_t, Epilogue::Store, false>(a, s);
+    return dispatch_small<bf16_t, Epilogue::Store>(a, s);
 }
 
 size_t fp8_hidden_scratch_bytes(Epilogue, int64_t rows, int n_groups, int K, int N) {
@@ -817,8 +821,8 @@ hipError_t launch_fp8_hidden(Epilogue epi, const Fp8GemmArgs& a, float* scratch,
     if (use_pp(a)) return swiglu ? run_pp<Epilogue::SwiGLU>(a, s) : run_pp<Epilogue::ReLU>(a, s);
     Fp8GemmArgs g = a;
     g.out = scratch;
-    const hipError_t e = swiglu ? dispatch_small<float, Epilogue::SwiGLU, false>(g, s)
-                                : dispatch_small<float, Epilogue::ReLU, false>(g, s);
+    const hipError_t e = swiglu ? dispatch_small<float, Epilogue::SwiGLU>(g, s)
+                                : dispatch_small<float, Epilogue::ReLU>(g, s);
     if (e != hipSuccess) return e;
     return launch_fp8_quantize(DType::F32, scratch, 1, static_cast<int>(a.rows), a.N, 1, a.out, a.out_scale, s);
 }
