@@ -562,13 +562,53 @@ ec2moe_status check_fp8_desc(const ec2moe_fp8_matmul_desc* d) {
 
 constexpr const char* kFp8MatmulName = "fp8_matmul";  // of the timing record; outside the layer step
 
+Fp8GemmArgs fp8_matmul_shape(const ec2moe_fp8_matmul_desc* d, const int32_t* seg) {
+    Fp8GemmArgs g{};
+    g.seg = seg; g.n_groups = d->n_groups; g.rows = d->rows; g.src_rows = d->rows; g.b_rows = d->n; g.K = d->k; g.N = d->n;
+    g.name = kFp8MatmulName;
+    return g;
+}
+
+// (float32 outputs take no split; either way of giving the segments may)
+size_t fp8_matmul_ws(const ec2moe_fp8_matmul_desc* d) {
+    if (d->out_dtype == EC2MOE_F32) return 0;
+    const int32_t some = 0;
+    return std::max(fp8_split_scratch_bytes(Epilogue::Store, fp8_matmul_shape(d, &some)),
+                    d->n_groups == 1 ? fp8_split_scratch_bytes(Epilogue::Store, fp8_matmul_shape(d, nullptr)) : 0);
+}
+
+// The two products of the expert networks, without their buffers.
+struct Fp8Experts {
+    Epilogue epi;
+    Fp8GemmArgs in, out;
+};
+
+Fp8Experts fp8_experts(const ec2moe_moe_desc* d, const int32_t* seg, const int32_t* perm_src) {
+    Fp8Experts x{};
+    const bool relu = (d->flags & EC2MOE_EXPERT_RELU) != 0;
+    const int64_t A = static_cast<int64_t>(d->n_tokens) * d->top_k;
+    x.epi = relu ? Epilogue::ReLU : Epilogue::SwiGLU;
+    Fp8GemmArgs& g = x.in;
+    g.seg = seg; g.row_index = perm_src; g.n_groups = d->n_experts; g.rows = A; g.src_rows = d->n_tokens;
+    g.b_rows = relu ? d->ffn_hidden : 2 * d->ffn_hidden; g.K = d->d_model; g.N = d->ffn_hidden;
+    g.name = relu ? "fp8_expert_in_relu" : "fp8_expert_gate_up";
+    Fp8GemmArgs& h = x.out;
+    h.seg = seg; h.n_groups = d->n_experts; h.rows = A; h.src_rows = A; h.b_rows = d->d_model; h.K = d->ffn_hidden;
+    h.N = d->d_model; h.name = "fp8_expert_down";
+    return x;
+}
+
 struct Fp8MoeWs {
-    size_t counts, seg, perm_src, inv_perm, xq, xs, act, act_q, act_s, y_perm, total;
+    size_t counts, seg, perm_src, inv_perm, xq, xs, act, act_q, act_s, y_perm, part, total;
+    bool split_in, split_out;
 };
 
 Fp8MoeWs fp8_moe_ws(const ec2moe_moe_desc* d) {
     const int64_t T = d->n_tokens, A = T * d->top_k, kb = d->d_model / kFp8Block, hb = d->ffn_hidden / kFp8Block;
-    const Epilogue epi = d->flags & EC2MOE_EXPERT_RELU ? Epilogue::ReLU : Epilogue::SwiGLU;
+    const int32_t some = 0;
+    const Fp8Experts x = fp8_experts(d, &some, &some);
+    const size_t part_in = fp8_split_scratch_bytes(x.epi, x.in);
+    const size_t part_out = d->dtype == EC2MOE_F32 ? 0 : fp8_split_scratch_bytes(Epilogue::Store, x.out);
     Fp8MoeWs w{};
     size_t o = 0;
     w.counts = o; o += up(static_cast<size_t>(std::max(1, perm_chunks(A))) * d->n_experts * 4);
@@ -577,10 +617,13 @@ Fp8MoeWs fp8_moe_ws(const ec2moe_moe_desc* d) {
     w.inv_perm = o; o += up(static_cast<size_t>(A) * 4);
     w.xq = o; o += up(static_cast<size_t>(T) * d->d_model);
     w.xs = o; o += up(static_cast<size_t>(T) * kb * 4);
-    w.act = o; o += up(fp8_hidden_scratch_bytes(epi, A, d->n_experts, d->d_model, d->ffn_hidden));
+    w.act = o; o += up(fp8_hidden_scratch_bytes(x.epi, x.in));
     w.act_q = o; o += up(static_cast<size_t>(A) * d->ffn_hidden);
     w.act_s = o; o += up(static_cast<size_t>(A) * hb * 4);
     w.y_perm = o; o += up(static_cast<size_t>(A) * d->d_model * elem_bytes(static_cast<DType>(d->dtype)));
+    w.part = o; o += up(std::max(part_in, part_out));
+    w.split_in = part_in > 0;
+    w.split_out = part_out > 0;
     w.total = o;
     return w;
 }
@@ -590,7 +633,7 @@ Fp8MoeWs fp8_moe_ws(const ec2moe_moe_desc* d) {
 ec2moe_status ec2moe_fp8_matmul_workspace_size(const ec2moe_fp8_matmul_desc* desc, size_t* bytes) {
     if (ec2moe_status st = check_fp8_desc(desc); st != EC2MOE_OK) return st;
     REQUIRE_PTR(bytes);
-    *bytes = 0;
+    *bytes = fp8_matmul_ws(desc);
     return ok();
 }
 
@@ -600,14 +643,15 @@ ec2moe_status ec2moe_fp8_matmul(const ec2moe_fp8_matmul_desc* desc, const void* 
     if (ec2moe_status st = check_fp8_desc(desc); st != EC2MOE_OK) return st;
     REQUIRE(seg_offsets != nullptr || desc->n_groups == 1, EC2MOE_ERR_INVALID_ARGUMENT,
             "seg_offsets is NULL with %d groups", desc->n_groups);
-    if (ec2moe_status st = check_ws(ws, ws_bytes, 0); st != EC2MOE_OK) return st;
+    const size_t need = fp8_matmul_ws(desc);
+    if (ec2moe_status st = check_ws(ws, ws_bytes, need); st != EC2MOE_OK) return st;
     if (desc->rows == 0) return ok();
     REQUIRE_PTR(a); REQUIRE_PTR(a_scale); REQUIRE_PTR(b); REQUIRE_PTR(b_scale); REQUIRE_PTR(out);
     REQUIRE_ALIGNED(a); REQUIRE_ALIGNED(a_scale); REQUIRE_ALIGNED(b); REQUIRE_ALIGNED(b_scale); REQUIRE_ALIGNED(out);
-    Fp8GemmArgs g{};
-    g.a = static_cast<const uint8_t*>(a); g.a_scale = a_scale; g.seg = seg_offsets; g.n_groups = desc->n_groups;
-    g.rows = desc->rows; g.src_rows = desc->rows; g.b = static_cast<const uint8_t*>(b); g.b_scale = b_scale;
-    g.b_rows = desc->n; g.K = desc->k; g.N = desc->n; g.out = out; g.name = kFp8MatmulName;
+    Fp8GemmArgs g = fp8_matmul_shape(desc, seg_offsets);
+    g.a = static_cast<const uint8_t*>(a); g.a_scale = a_scale; g.b = static_cast<const uint8_t*>(b); g.b_scale = b_scale;
+    g.out = out;
+    if (need && fp8_split_scratch_bytes(Epilogue::Store, g)) g.part = static_cast<float*>(ws);
     return hip_status(launch_fp8_gemm(static_cast<DType>(desc->out_dtype), g, stream), "fp8_matmul launch");
 }
 
@@ -633,7 +677,6 @@ ec2moe_status ec2moe_fp8_moe_forward(const ec2moe_moe_desc* desc, const void* x,
     const DType dt = static_cast<DType>(desc->dtype);
     const int T = desc->n_tokens, d = desc->d_model, H = desc->ffn_hidden, M = desc->n_experts;
     const int64_t A = static_cast<int64_t>(T) * desc->top_k;
-    const bool relu = (desc->flags & EC2MOE_EXPERT_RELU) != 0;
     REQUIRE(fp8_gemm_fits(A, M, H) && fp8_gemm_fits(A, M, d), EC2MOE_ERR_UNSUPPORTED,
             "%lld assignments are too many for one launch", static_cast<long long>(A));
     int32_t* seg = at<int32_t>(ws, w.seg);
@@ -642,19 +685,19 @@ ec2moe_status ec2moe_fp8_moe_forward(const ec2moe_moe_desc* desc, const void* x,
     hipError_t e = launch_permute(topk_idx, A, desc->top_k, M, at<int32_t>(ws, w.counts), seg, perm_src, inv_perm,
                                   stream);
     if (e == hipSuccess) e = launch_fp8_quantize(dt, x, 1, T, d, 1, at<void>(ws, w.xq), at<float>(ws, w.xs), stream);
+    Fp8Experts x8 = fp8_experts(desc, seg, perm_src);
     if (e == hipSuccess) {
-        Fp8GemmArgs g{};
-        g.a = at<uint8_t>(ws, w.xq); g.a_scale = at<float>(ws, w.xs); g.row_index = perm_src; g.seg = seg;
-        g.n_groups = M; g.rows = A; g.src_rows = T; g.b = static_cast<const uint8_t*>(w_gate_up);
-        g.b_scale = w_gate_up_scale; g.b_rows = relu ? H : 2 * H; g.K = d; g.N = H; g.out = at<void>(ws, w.act_q);
-        g.out_scale = at<float>(ws, w.act_s); g.name = relu ? "fp8_expert_in_relu" : "fp8_expert_gate_up";
-        e = launch_fp8_hidden(relu ? Epilogue::ReLU : Epilogue::SwiGLU, g, at<float>(ws, w.act), stream);
+        Fp8GemmArgs& g = x8.in;
+        g.a = at<uint8_t>(ws, w.xq); g.a_scale = at<float>(ws, w.xs); g.b = static_cast<const uint8_t*>(w_gate_up);
+        g.b_scale = w_gate_up_scale; g.out = at<void>(ws, w.act_q); g.out_scale = at<float>(ws, w.act_s);
+        if (w.split_in) g.part = at<float>(ws, w.part);
+        e = launch_fp8_hidden(x8.epi, g, at<float>(ws, w.act), stream);
     }
     if (e == hipSuccess) {
-        Fp8GemmArgs g{};
-        g.a = at<uint8_t>(ws, w.act_q); g.a_scale = at<float>(ws, w.act_s); g.seg = seg; g.n_groups = M; g.rows = A;
-        g.src_rows = A; g.b = static_cast<const uint8_t*>(w_down); g.b_scale = w_down_scale; g.b_rows = d; g.K = H;
-        g.N = d; g.out = at<void>(ws, w.y_perm); g.name = "fp8_expert_down";
+        Fp8GemmArgs& g = x8.out;
+        g.a = at<uint8_t>(ws, w.act_q); g.a_scale = at<float>(ws, w.act_s); g.b = static_cast<const uint8_t*>(w_down);
+        g.b_scale = w_down_scale; g.out = at<void>(ws, w.y_perm);
+        if (w.split_out) g.part = at<float>(ws, w.part);
         e = launch_fp8_gemm(dt, g, stream);
     }
     if (e == hipSuccess)

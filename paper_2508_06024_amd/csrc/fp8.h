@@ -32,6 +32,7 @@ struct Fp8GemmArgs {
     int K, N;
     void* out;                // [rows][N]
     float* out_scale;         // [rows][N / 128] (hidden rows)
+    float* part;              // fp8_split_scratch_bytes() of scratch, or null: the last round is not split along K
     const char* name;         // kernel name for the timing record
 };
 // Largest number of tiles of a launch (see fp8_gemm.hip): larger products are refused.
@@ -43,7 +44,10 @@ hipError_t launch_fp8_gemm(DType out_type, const Fp8GemmArgs& a, hipStream_t s);
 // Hidden rows of the experts: SwiGLU (weight rows 0..N-1 are the gate branch and N..2N-1 the up branch), silu(gate)
 // * up, or ReLU, max(sum, 0); N and K multiples of 128. Quantised by rows from their float32 values to out and
 // out_scale, by way of scratch (fp8_hidden_scratch_bytes) where the product's tiles do not hold whole blocks.
-size_t fp8_hidden_scratch_bytes(Epilogue epi, int64_t rows, int n_groups, int K, int N);
 hipError_t launch_fp8_hidden(Epilogue epi, const Fp8GemmArgs& a, float* scratch, hipStream_t s);
+
+// Scratch of a product, from the shape fields of its arguments and whether they have seg and row_index.
+size_t fp8_hidden_scratch_bytes(Epilogue epi, const Fp8GemmArgs& a);
+size_t fp8_split_scratch_bytes(Epilogue epi, const Fp8GemmArgs& a);
 
 }  // namespace ec2moe

@@ -17,11 +17,15 @@
 #include "fp8_device.h"
 #include "gemm_tiles.h"
 
+#include <cmath>
+#include <string>
+
 namespace ec2moe {
 namespace {
 
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(4))) float cfloat;  // constant memory
+constexpr int kSplitSlots = 256;                         // workgroups of the 256 x 256 kernel, one per CU
 
 __device__ __forceinline__ float relu(float v) { return v < 0.f ? 0.f : v; }  // NaN stays
 
@@ -374,24 +378,29 @@ __global__ __launch_bounds__(512, 1) void fp8_pp_kernel(Fp8GemmArgs p) {
     __shared__ __attribute__((aligned(1024))) char w2[SLOT];
 
     const int ntn = (p.N + NOUT - 1) / NOUT;
-    const int K = p.K, nk = K / kFp8Block;
-    constexpr int P = 256;           // workgroups, one per CU
+    const int K = p.K, nk_all = K / kFp8Block;
+    constexpr int P = kSplitSlots;   // workgroups, one per CU
     constexpr int XW = P / kXcds;
-    const int total = count_tiles<TM>(p, ntn);
-    const int rounds = total / P;
+    const SplitPlan sp = split_plan(count_tiles<TM>(p, ntn), P, p.part ? kMaxSplitChunks : 1, nk_all);
+    const int rounds = sp.full / P;
     const int wg = blockIdx.x;
 
     // whole rounds first, each XCD's workgroups stepping through consecutive tiles; then the tail
     for (int it = 0; it <= rounds; ++it) {
-    int bid;
+    int bid, chunk = 0;
+    bool split = false;
     if (it < rounds) {
         bid = (wg % kXcds) * (rounds * XW) + it * XW + wg / kXcds;
     } else {
-        bid = rounds * P + wg;
-        if (bid >= total) break;
+        if (wg >= sp.tail * sp.S) break;
+        bid = sp.full + wg / sp.S;
+        chunk = wg % sp.S;
+        split = sp.S > 1;
     }
     TileInfo ti;
     if (!tile_of<TM>(p, ntn, bid, ti)) break;
+    const int kb = split ? chunk * sp.chunk_slabs : 0;  // first slab of this unit
+    const int nk = split ? std::min(nk_all, kb + sp.chunk_slabs) - kb : nk_all;
 
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));
@@ -424,7 +433,7 @@ __global__ __launch_bounds__(512, 1) void fp8_pp_kernel(Fp8GemmArgs p) {
         for (int i = 0; i < LOADS; ++i) {
             lds_void* dst = reinterpret_cast<lds_void*>(
                 reinterpret_cast<uintptr_t>(slot + ((wave & 3) * WROWS + i * 8) * RB));
-            raw_buffer_load_lds(rs, dst, 16, static_cast<int>(voff[i]), ks * RB, 0, 0);
+            raw_buffer_load_lds(rs, dst, 16, static_cast<int>(voff[i]), (kb + ks) * RB, 0, 0);
         }
     };
 
@@ -449,19 +458,19 @@ __global__ __launch_bounds__(512, 1) void fp8_pp_kernel(Fp8GemmArgs p) {
     uint32_t tso;
     {
         const int64_t pos = ti.row0 + std::min(wm * WTOK + lane, ti.valid - 1);
-        tso = static_cast<uint32_t>(p.row_index ? p.row_index[pos] : pos) * static_cast<uint32_t>(4 * nk);
+        tso = static_cast<uint32_t>(p.row_index ? p.row_index[pos] : pos) * static_cast<uint32_t>(4 * nk_all);
         asm volatile("" : "+v"(tso));
     }
-    const float* sg = p.b_scale + static_cast<int64_t>(ti.group) * scale_rows(p) * nk;
-    const cfloat* ws0 = (const cfloat*)(sg + static_cast<int64_t>(uniform(weight_row<TN, SWIGLU>(p, ti.nt, wn * WW) / kFp8Block)) * nk);
+    const float* sg = p.b_scale + static_cast<int64_t>(ti.group) * scale_rows(p) * nk_all;
+    const cfloat* ws0 = (const cfloat*)(sg + static_cast<int64_t>(uniform(weight_row<TN, SWIGLU>(p, ti.nt, wn * WW) / kFp8Block)) * nk_all + kb);
     const cfloat* ws1 =
-        (const cfloat*)(sg + static_cast<int64_t>(uniform(weight_row<TN, SWIGLU>(p, ti.nt, TN / 2 + wn * WW) / kFp8Block)) * nk);
+        (const cfloat*)(sg + static_cast<int64_t>(uniform(weight_row<TN, SWIGLU>(p, ti.nt, TN / 2 + wn * WW) / kFp8Block)) * nk_all + kb);
     struct Scales {
         float t, w0, w1;
     };
     auto load_scales = [&](int ks) {
         Scales s;
-        s.t = *reinterpret_cast<const float*>(reinterpret_cast<const char*>(p.a_scale + ks) + tso);
+        s.t = *reinterpret_cast<const float*>(reinterpret_cast<const char*>(p.a_scale + kb + ks) + tso);
         s.w0 = ws0[ks];
         s.w1 = SWIGLU ? ws1[ks] : 0.f;
         return s;
@@ -548,7 +557,9 @@ __global__ __launch_bounds__(512, 1) void fp8_pp_kernel(Fp8GemmArgs p) {
     };
 
     // slab s: tokens in slot s % 2, weights in slot s % 3 (the loops run six slabs a turn)
-    if (tok_wave) {
+    if (nk <= 0) {
+        // a chunk past the end of K (whole pairs of slabs a chunk): zeros
+    } else if (tok_wave) {
         Scales nxt = load_scales(0);
         issue_slab(0, t0);
         __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
@@ -586,8 +597,9 @@ __global__ __launch_bounds__(512, 1) void fp8_pp_kernel(Fp8GemmArgs p) {
         Frags f;
         __builtin_amdgcn_sched_barrier(0);
         issue_slab(0, w0);
-        issue_slab(1, w1);  // nk >= 2 on this path
-        __builtin_amdgcn_s_waitcnt(vmcnt_imm(LOADS));  // own rows of slab 0 landed
+        if (nk > 1) issue_slab(1, w1);
+        if (nk > 1) __builtin_amdgcn_s_waitcnt(vmcnt_imm(LOADS));  // own rows of slab 0 landed
+        else __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
         barrier();
         // Memory phase of slab s. The slot refilled in it holds slab s - 1, whose last reads (this group's) were
         // done before the barrier ahead of it: no wave can still be reading it.
@@ -630,6 +642,19 @@ __global__ __launch_bounds__(512, 1) void fp8_pp_kernel(Fp8GemmArgs p) {
         mma_slab(last == 0 ? w0 : last == 1 ? w1 : w2, f, sc);
     }
 
+    if (split) {
+        // float32 sums [TM][TN] (weight rows in tile order) of this chunk of K; lane l holds, per block, weight rows
+        // 4 (l / 16) .. + 3 of token row l % 16
+        float* part = p.part + static_cast<int64_t>(wg) * TM * TN;
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) {
+            const int trow = wm * WTOK + mi * 16 + l16;
+#pragma unroll
+            for (int ni = 0; ni < NI; ++ni)
+                *reinterpret_cast<f32x4*>(part + trow * TN + wn * WW + wblk(ni) + 4 * lg) = acc[ni][mi];
+        }
+        break;  // the last unit of the workgroup
+    }
     // The finished tile is staged in LDS so that the global stores are whole rows: 16 bytes per lane. Token
     // slots are free after the last slab; weight slots once the weight loaders' last products are done.
     if constexpr (QUANT) {
@@ -733,6 +758,52 @@ __global__ __launch_bounds__(512, 1) void fp8_pp_kernel(Fp8GemmArgs p) {
     }
 }
 
+// Sums the partial tiles of the split tail in chunk order and finishes them like the kernel above. One workgroup per (tail
+// tile, 16 rows); a thread owns 4 output columns, 32 threads a block of 128 of a row.
+template <Epilogue EPI>
+__global__ __launch_bounds__(256) void fp8_split_reduce_kernel(Fp8GemmArgs p) {
+    constexpr bool SWIGLU = EPI == Epilogue::SwiGLU;
+    constexpr int TM = 256, TN = 256, NOUT = SWIGLU ? TN / 2 : TN, QUADS = NOUT / 4, ROWS = 16;
+    const int ntn = (p.N + NOUT - 1) / NOUT;
+    const SplitPlan sp = split_plan(count_tiles<TM>(p, ntn), kSplitSlots, kMaxSplitChunks, p.K / kFp8Block);
+    const int t = blockIdx.x / (TM / ROWS);
+    if (sp.S <= 1 || t >= sp.tail) return;
+    TileInfo ti;
+    if (!tile_of<TM>(p, ntn, sp.full + t, ti)) return;
+    const float* tile = p.part + static_cast<int64_t>(t) * sp.S * TM * TN;
+    const int r0 = (blockIdx.x % (TM / ROWS)) * ROWS;
+    for (int i = threadIdx.x; i < ROWS * QUADS; i += 256) {
+        const int r = r0 + i / QUADS, c = i % QUADS * 4;
+        f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f}, u = v;
+#pragma unroll 4
+        for (int k = 0; k < sp.S; ++k) {
+            const float* src = tile + (static_cast<int64_t>(k) * TM + r) * TN + c;
+            v += *reinterpret_cast<const f32x4*>(src);
+            if (SWIGLU) u += *reinterpret_cast<const f32x4*>(src + TN / 2);
+        }
+        const int col = ti.nt * NOUT + c;
+        const bool keep = r < ti.valid && col < p.N;
+        if constexpr (EPI == Epilogue::Store) {
+            if (keep) store_run(static_cast<bf16_t*>(p.out) + (ti.row0 + r) * p.N + col, v, 4, true);
+        } else {
+            uint32_t m = 0;
+            float f[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                f[e] = SWIGLU ? silu(v[e]) * u[e] : relu(v[e]);
+                m = max(m, magnitude(f[e]));
+            }
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), off)));
+            const BlockScale bs = block_scale(m);
+            const uint32_t q = quantize4(f, bs);
+            if (!keep) continue;
+            *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(p.out) + (ti.row0 + r) * p.N + col) = q;
+            if (c % kFp8Block == 0) p.out_scale[(ti.row0 + r) * (p.N / kFp8Block) + col / kFp8Block] = bs.scale;
+        }
+    }
+}
+
 // ------------------------------------------------------------------ dispatch
 
 // Tiles of a launch at most: a group of r rows has ceil(r / TM) <= r / TM + 1 of them per column tile.
@@ -763,8 +834,16 @@ hipError_t run_ring(const Fp8GemmArgs& a, hipStream_t s) {
 
 template <Epilogue EPI>
 hipError_t run_pp(const Fp8GemmArgs& a, hipStream_t s) {
-    ProfileScope prof(a.name, s);
-    hipLaunchKernelGGL((fp8_pp_kernel<EPI>), dim3(256), dim3(512), 0, s, a);
+    {
+        ProfileScope prof(a.name, s);
+        hipLaunchKernelGGL((fp8_pp_kernel<EPI>), dim3(kSplitSlots), dim3(512), 0, s, a);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !a.part) return e;
+    // a tail is split into two chunks or more: at most half a round of tiles
+    const std::string name = std::string(a.name) + "_tail";
+    ProfileScope prof(name.c_str(), s);
+    hipLaunchKernelGGL((fp8_split_reduce_kernel<EPI>), dim3(kSplitSlots / 2 * 16), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
@@ -775,8 +854,27 @@ bool offsets32(const Fp8GemmArgs& a) {
     return (!a.row_index || a.src_rows * a.K < (int64_t(1) << 32)) && a.src_rows * (a.K / kFp8Block) * 4 < (int64_t(1) << 32);
 }
 
-bool use_pp(const Fp8GemmArgs& a) {
-    return offsets32(a) && avg_rows(a) >= 256 && a.K >= 2 * kFp8Block;
+// Rounds of the machine that tiles of tm x tn take, `slots` at a time: full tiles and half of another per group that has
+// rows (the segments' lengths are on the device).
+double rounds(const Fp8GemmArgs& a, int tm, int tn, int slots) {
+    const int64_t active = std::min<int64_t>(a.rows, a.n_groups);
+    const int64_t mt = a.seg ? std::max(active, a.rows / tm + active / 2) : (a.rows + tm - 1) / tm;
+    return std::ceil(static_cast<double>(mt * ((a.N + tn - 1) / tn)) / slots);
+}
+
+// Whether the last round of the 256 x 256 tiles may be worth splitting along K: long K, and rounds few enough that it weighs.
+// (Whether it is split, and into how many chunks, follows from the number of tiles, on the device.)
+bool may_split(const Fp8GemmArgs& a, bool swiglu) {
+    return a.K >= 16 * kFp8Block && rounds(a, 256, swiglu ? 128 : 256, 1) <= 8 * kSplitSlots;
+}
+
+// The 256 x 256 tiles where their rounds cost less than those of the ring's 64-row ones: a block of K takes about 2.5 us a
+// round (256 tiles, however many of their rows are real: the rate of the weights), 1.9 us a round of the ring's (512).
+// 16 experts, 2048 -> 4096 -> 2048: 133 us with the ring, 155 with them at 32 rows an expert, 173 and 153 at 64, 271 and
+// 160 at 128; 64 experts, 1024 -> 2048 -> 1024: 129 and 158, 191 and 162, 288 and 177.
+bool use_pp(const Fp8GemmArgs& a, bool swiglu) {
+    return offsets32(a) && a.K >= 2 * kFp8Block &&
+           2.5 * rounds(a, 256, swiglu ? 128 : 256, 256) <= 1.9 * rounds(a, 64, swiglu ? 64 : 128, 512);
 }
 
 template <typename TO, Epilogue EPI>
@@ -802,23 +900,23 @@ bool fp8_gemm_fits(int64_t rows, int n_groups, int64_t n) {
 hipError_t launch_fp8_gemm(DType out_type, const Fp8GemmArgs& a, hipStream_t s) {
     if (a.rows == 0) return hipSuccess;
     if (out_type == DType::F32) return dispatch_small<float, Epilogue::Store>(a, s);
-    if (use_pp(a) && a.N % 8 == 0) return run_pp<Epilogue::Store>(a, s);
+    if (use_pp(a, false) && a.N % 8 == 0) return run_pp<Epilogue::Store>(a, s);
     return dispatch_small<bf16_t, Epilogue::Store>(a, s);
 }
 
-size_t fp8_hidden_scratch_bytes(Epilogue, int64_t rows, int n_groups, int K, int N) {
-    Fp8GemmArgs a{};
-    a.rows = rows;
-    a.n_groups = n_groups;
-    a.K = K;
-    a.N = N;
-    return use_pp(a) ? 0 : static_cast<size_t>(rows) * N * sizeof(float);
+size_t fp8_split_scratch_bytes(Epilogue epi, const Fp8GemmArgs& a) {
+    const bool swiglu = epi == Epilogue::SwiGLU;
+    return use_pp(a, swiglu) && may_split(a, swiglu) ? static_cast<size_t>(kSplitSlots) * 256 * 256 * sizeof(float) : 0;
+}
+
+size_t fp8_hidden_scratch_bytes(Epilogue epi, const Fp8GemmArgs& a) {
+    return use_pp(a, epi == Epilogue::SwiGLU) ? 0 : static_cast<size_t>(a.rows) * a.N * sizeof(float);
 }
 
 hipError_t launch_fp8_hidden(Epilogue epi, const Fp8GemmArgs& a, float* scratch, hipStream_t s) {
     if (a.rows == 0) return hipSuccess;
     const bool swiglu = epi == Epilogue::SwiGLU;
-    if (use_pp(a)) return swiglu ? run_pp<Epilogue::SwiGLU>(a, s) : run_pp<Epilogue::ReLU>(a, s);
+    if (use_pp(a, swiglu)) return swiglu ? run_pp<Epilogue::SwiGLU>(a, s) : run_pp<Epilogue::ReLU>(a, s);
     Fp8GemmArgs g = a;
     g.out = scratch;
     const hipError_t e = swiglu ? dispatch_small<float, Epilogue::SwiGLU>(g, s)
