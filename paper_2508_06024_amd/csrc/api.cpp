@@ -599,8 +599,8 @@ Fp8Experts fp8_experts(const ec2moe_moe_desc* d, const int32_t* seg, const int32
 }
 
 struct Fp8MoeWs {
-    size_t counts, seg, perm_src, inv_perm, xq, xs, act, act_q, act_s, y_perm, part, total;
-    bool split_in, split_out;
+    size_t counts, seg, perm_src, inv_perm, xq, xs, act, act_q, act_s, y_perm, y_scale, part, total;
+    bool split_in, split_out, half;  // half: y_perm as float16 with scales, else float32
 };
 
 Fp8MoeWs fp8_moe_ws(const ec2moe_moe_desc* d) {
@@ -620,7 +620,9 @@ Fp8MoeWs fp8_moe_ws(const ec2moe_moe_desc* d) {
     w.act = o; o += up(fp8_hidden_scratch_bytes(x.epi, x.in));
     w.act_q = o; o += up(static_cast<size_t>(A) * d->ffn_hidden);
     w.act_s = o; o += up(static_cast<size_t>(A) * hb * 4);
-    w.y_perm = o; o += up(static_cast<size_t>(A) * d->d_model * elem_bytes(static_cast<DType>(d->dtype)));
+    w.half = d->dtype == EC2MOE_BF16 && fp8_rows_half(x.out);
+    w.y_perm = o; o += up(static_cast<size_t>(A) * d->d_model * (w.half ? 2 : 4));
+    w.y_scale = o; o += up(w.half ? static_cast<size_t>(A) * kb * 4 : 0);
     w.part = o; o += up(std::max(part_in, part_out));
     w.split_in = part_in > 0;
     w.split_out = part_out > 0;
@@ -696,12 +698,14 @@ ec2moe_status ec2moe_fp8_moe_forward(const ec2moe_moe_desc* desc, const void* x,
     if (e == hipSuccess) {
         Fp8GemmArgs& g = x8.out;
         g.a = at<uint8_t>(ws, w.act_q); g.a_scale = at<float>(ws, w.act_s); g.b = static_cast<const uint8_t*>(w_down);
-        g.b_scale = w_down_scale; g.out = at<void>(ws, w.y_perm);
+        g.b_scale = w_down_scale; g.out = at<void>(ws, w.y_perm); g.out_scale = at<float>(ws, w.y_scale);
         if (w.split_out) g.part = at<float>(ws, w.part);
-        e = launch_fp8_gemm(dt, g, stream);
+        e = dt == DType::F32 ? launch_fp8_gemm(dt, g, stream) : launch_fp8_rows(g, stream);
     }
     if (e == hipSuccess)
-        e = launch_combine(dt, at<void>(ws, w.y_perm), inv_perm, topk_w, T, desc->top_k, d, y, stream);
+        e = dt == DType::F32 ? launch_combine(dt, at<void>(ws, w.y_perm), inv_perm, topk_w, T, desc->top_k, d, y, stream)
+                             : launch_fp8_combine(at<void>(ws, w.y_perm), w.half ? at<float>(ws, w.y_scale) : nullptr, inv_perm,
+                                                  topk_w, T, desc->top_k, d, y, stream);
     return hip_status(e, "fp8_moe_forward launch");
 }
 

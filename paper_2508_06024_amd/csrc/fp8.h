@@ -31,7 +31,7 @@ struct Fp8GemmArgs {
     int b_rows;
     int K, N;
     void* out;                // [rows][N]
-    float* out_scale;         // [rows][N / 128] (hidden rows)
+    float* out_scale;         // [rows][N / 128] (hidden rows, float16 rows)
     float* part;              // fp8_split_scratch_bytes() of scratch, or null: the last round is not split along K
     const char* name;         // kernel name for the timing record
 };
@@ -45,6 +45,14 @@ hipError_t launch_fp8_gemm(DType out_type, const Fp8GemmArgs& a, hipStream_t s);
 // * up, or ReLU, max(sum, 0); N and K multiples of 128. Quantised by rows from their float32 values to out and
 // out_scale, by way of scratch (fp8_hidden_scratch_bytes) where the product's tiles do not hold whole blocks.
 hipError_t launch_fp8_hidden(Epilogue epi, const Fp8GemmArgs& a, float* scratch, hipStream_t s);
+
+// Rows for launch_fp8_combine (N a multiple of 128): float16 with a scale per 128 columns in out_scale where
+// fp8_rows_half(), else float32.
+bool fp8_rows_half(const Fp8GemmArgs& a);
+hipError_t launch_fp8_rows(const Fp8GemmArgs& a, hipStream_t s);
+// y[t] (bfloat16) = sum over k slots of w times the rows, which have scales or are float32 (scale null)
+hipError_t launch_fp8_combine(const void* rows, const float* scale, const int32_t* inv_perm, const float* w, int n_tokens,
+                              int top_k, int d, void* y, hipStream_t s);
 
 // Scratch of a product, from the shape fields of its arguments and whether they have seg and row_index.
 size_t fp8_hidden_scratch_bytes(Epilogue epi, const Fp8GemmArgs& a);

@@ -52,6 +52,20 @@ __device__ __forceinline__ uint32_t quantize4(const float* x, const BlockScale& 
 
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
+// ------------------------------------------------------------------ float16 rows
+//
+// The power of two that brings values of magnitude up to `bits` into [2^14, 2^15), and its inverse: float16 then keeps
+// 11 bits of the largest and of everything down to 2^-28 of it. With an infinity or NaN among them both are 1.
+struct HalfScale {
+    float scale, inv;
+};
+__device__ __forceinline__ HalfScale half_scale(uint32_t bits) {
+    const uint32_t e = bits >> 23;
+    if (e == 255) return {1.f, 1.f};
+    const uint32_t c = max(e, 15u);
+    return {__uint_as_float((c - 14u) << 23), __uint_as_float((268u - c) << 23)};
+}
+
 // ------------------------------------------------------------------ products of a block of 128
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));

@@ -24,6 +24,7 @@ namespace ec2moe {
 namespace {
 
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(4))) float cfloat;  // constant memory
 constexpr int kSplitSlots = 256;                         // workgroups of the 256 x 256 kernel, one per CU
 
@@ -354,10 +355,10 @@ __global__ __launch_bounds__(256, 2) void fp8_ring_kernel(Fp8GemmArgs p) {
 // block's 32 bytes a lane are read AHEAD blocks of products ahead, behind the same barriers. Scales are loaded a slab
 // ahead and before the slab loads of the phase, so that its counted waits cover them. The 128
 // scaling multiply-adds of a slab issue under its products (16 of every 32 cycles).
-// EPI Store writes bfloat16 rows. SwiGLU and ReLU quantise: a tile holds one (ReLU: two) whole blocks of 128
+// EPI Store writes bfloat16 rows, or (HALF) float16 rows with a power-of-two scale for each 128 columns, a wave's. SwiGLU and ReLU quantise: a tile holds one (ReLU: two) whole blocks of 128
 // hidden columns of each row, whose largest value meets across the lanes and, with SwiGLU, the two
 // waves of the row.
-template <Epilogue EPI>
+template <Epilogue EPI, bool HALF = false>
 __global__ __launch_bounds__(512, 1) void fp8_pp_kernel(Fp8GemmArgs p) {
     constexpr bool SWIGLU = EPI == Epilogue::SwiGLU;
     constexpr bool QUANT = EPI != Epilogue::Store;
@@ -446,8 +447,7 @@ __global__ __launch_bounds__(512, 1) void fp8_pp_kernel(Fp8GemmArgs p) {
     const int off_w = (wn * WW + l16) * RB;    // in a weight slot
     auto wblk = [](int ni) constexpr {
         if (SWIGLU) {
-            constexpr int HALF = NI / 2;
-            return (ni < HALF ? 0 : TN / 2) + (ni % HALF) * 16;
+            return (ni < NI / 2 ? 0 : TN / 2) + (ni % (NI / 2)) * 16;
         }
         return ni * 16;
     };
@@ -729,14 +729,37 @@ __global__ __launch_bounds__(512, 1) void fp8_pp_kernel(Fp8GemmArgs p) {
         for (int mi = 0; mi < MI; ++mi) {
             const int r = mi * 16 + l16;
             const int sr = wm * WTOK + r;
+            HalfScale hs{1.f, 1.f};
+            if constexpr (HALF) {
+                uint32_t m = 0;
+#pragma unroll
+                for (int ni = 0; ni < NI; ++ni)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) m = max(m, magnitude(acc[ni][mi][e]));
+                m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 16)));
+                m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 32)));
+                hs = half_scale(m);
+                const int blk = ti.nt * WN + wn;
+                if (lg == 0 && sr < ti.valid && blk < p.N / kFp8Block)
+                    p.out_scale[(ti.row0 + sr) * (p.N / kFp8Block) + blk] = hs.scale;
+            }
 #pragma unroll
             for (int ni = 0; ni < NI; ++ni) {
-                bf16x4 o;
+                uint2 o;
+                if constexpr (HALF) {
+                    f16x4 h;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = static_cast<__bf16>(acc[ni][mi][e]);
+                    for (int e = 0; e < 4; ++e) h[e] = static_cast<_Float16>(acc[ni][mi][e] * hs.inv);
+                    o = __builtin_bit_cast(uint2, h);
+                } else {
+                    bf16x4 h;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) h[e] = static_cast<__bf16>(acc[ni][mi][e]);
+                    o = __builtin_bit_cast(uint2, h);
+                }
                 const int col = wn * (NOUT / WN) + ni * 16 + 8 * (lg >> 1);
                 const int ch = (col / 8) ^ (sr % OCH);
-                *reinterpret_cast<bf16x4*>(wst + r * OROW + ch * 16 + (lg & 1) * 8) = o;
+                *reinterpret_cast<uint2*>(wst + r * OROW + ch * 16 + (lg & 1) * 8) = o;
             }
         }
         __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
@@ -760,7 +783,7 @@ __global__ __launch_bounds__(512, 1) void fp8_pp_kernel(Fp8GemmArgs p) {
 
 // Sums the partial tiles of the split tail in chunk order and finishes them like the kernel above. One workgroup per (tail
 // tile, 16 rows); a thread owns 4 output columns, 32 threads a block of 128 of a row.
-template <Epilogue EPI>
+template <Epilogue EPI, bool HALF>
 __global__ __launch_bounds__(256) void fp8_split_reduce_kernel(Fp8GemmArgs p) {
     constexpr bool SWIGLU = EPI == Epilogue::SwiGLU;
     constexpr int TM = 256, TN = 256, NOUT = SWIGLU ? TN / 2 : TN, QUADS = NOUT / 4, ROWS = 16;
@@ -783,7 +806,20 @@ __global__ __launch_bounds__(256) void fp8_split_reduce_kernel(Fp8GemmArgs p) {
         }
         const int col = ti.nt * NOUT + c;
         const bool keep = r < ti.valid && col < p.N;
-        if constexpr (EPI == Epilogue::Store) {
+        if constexpr (HALF) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m = max(m, magnitude(v[e]));
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), off)));
+            const HalfScale hs = half_scale(m);
+            f16x4 h;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[e] = static_cast<_Float16>(v[e] * hs.inv);
+            if (!keep) continue;
+            *reinterpret_cast<f16x4*>(static_cast<_Float16*>(p.out) + (ti.row0 + r) * p.N + col) = h;
+            if (c % kFp8Block == 0) p.out_scale[(ti.row0 + r) * (p.N / kFp8Block) + col / kFp8Block] = hs.scale;
+        } else if constexpr (EPI == Epilogue::Store) {
             if (keep) store_run(static_cast<bf16_t*>(p.out) + (ti.row0 + r) * p.N + col, v, 4, true);
         } else {
             uint32_t m = 0;
@@ -832,18 +868,18 @@ hipError_t run_ring(const Fp8GemmArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
-template <Epilogue EPI>
+template <Epilogue EPI, bool HALF = false>
 hipError_t run_pp(const Fp8GemmArgs& a, hipStream_t s) {
     {
         ProfileScope prof(a.name, s);
-        hipLaunchKernelGGL((fp8_pp_kernel<EPI>), dim3(kSplitSlots), dim3(512), 0, s, a);
+        hipLaunchKernelGGL((fp8_pp_kernel<EPI, HALF>), dim3(kSplitSlots), dim3(512), 0, s, a);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.part) return e;
     // a tail is split into two chunks or more: at most half a round of tiles
     const std::string name = std::string(a.name) + "_tail";
     ProfileScope prof(name.c_str(), s);
-    hipLaunchKernelGGL((fp8_split_reduce_kernel<EPI>), dim3(kSplitSlots / 2 * 16), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((fp8_split_reduce_kernel<EPI, HALF>), dim3(kSplitSlots / 2 * 16), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
@@ -902,6 +938,13 @@ hipError_t launch_fp8_gemm(DType out_type, const Fp8GemmArgs& a, hipStream_t s) 
     if (out_type == DType::F32) return dispatch_small<float, Epilogue::Store>(a, s);
     if (use_pp(a, false) && a.N % 8 == 0) return run_pp<Epilogue::Store>(a, s);
     return dispatch_small<bf16_t, Epilogue::Store>(a, s);
+}
+
+bool fp8_rows_half(const Fp8GemmArgs& a) { return use_pp(a, false); }
+
+hipError_t launch_fp8_rows(const Fp8GemmArgs& a, hipStream_t s) {
+    if (a.rows == 0) return hipSuccess;
+    return fp8_rows_half(a) ? run_pp<Epilogue::Store, true>(a, s) : dispatch_small<float, Epilogue::Store>(a, s);
 }
 
 size_t fp8_split_scratch_bytes(Epilogue epi, const Fp8GemmArgs& a) {

@@ -63,7 +63,7 @@ STAGE_OF_KERNEL = {
     "codec_decode": "decode",
     "expert_gate_up": "expert_gate_up", "expert_in_relu": "expert_in_relu", "expert_down": "expert_down",
     "fp8_quantize_rows": "permute", "fp8_expert_gate_up": "expert_gate_up", "fp8_expert_in_relu": "expert_in_relu",
-    "fp8_expert_down": "expert_down",
+    "fp8_expert_down": "expert_down", "fp8_combine": "combine",
     "combine": "combine",
 }
 
