@@ -50,6 +50,26 @@ __device__ __forceinline__ void store_run(TO* dst, f32x4 v, int left, bool whole
         if (i < left) dst[i] = Elem<TO>::from_f32(v[i]);
 }
 
+// out[mi] of every lane = v of lane 16 mi + lane % 16 (MI 2: the upper half of the wave holds the lower one's values)
+template <int MI>
+__device__ __forceinline__ void spread(float v, float (&out)[MI]) {
+    static_assert(MI == 2 || MI == 4, "a row of the wave per block of 16");
+    typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+    const uint32_t u = __float_as_uint(v);
+    const u32x2 r = __builtin_amdgcn_permlane16_swap(u, u, false, false);  // rows 0 0 2 2, 1 1 3 3
+    if constexpr (MI == 2) {
+        out[0] = __uint_as_float(r[0]);
+        out[1] = __uint_as_float(r[1]);
+    } else {
+        const u32x2 e = __builtin_amdgcn_permlane32_swap(r[0], r[0], false, false);  // rows 0 0 0 0, 2 2 2 2
+        const u32x2 o = __builtin_amdgcn_permlane32_swap(r[1], r[1], false, false);
+        out[0] = __uint_as_float(e[0]);
+        out[1] = __uint_as_float(o[0]);
+        out[2] = __uint_as_float(e[1]);
+        out[3] = __uint_as_float(o[1]);
+    }
+}
+
 // ------------------------------------------------------------------ few rows
 //
 // A tile of 16 MT token rows and 16 NT weight rows (SwiGLU: NT gate and NT up blocks) by WAVES waves that
@@ -229,16 +249,17 @@ __global__ __launch_bounds__(256, 2) void fp8_ring_kernel(Fp8GemmArgs p) {
         }
     };
 
-    // scales: a token row's per lane, one (SwiGLU: two) of the weights for the tile
-    const float* tsc[MI];
-#pragma unroll
-    for (int mi = 0; mi < MI; ++mi) {
-        const int64_t pos = ti.row0 + std::min(mi * 16 + l16, ti.valid - 1);
-        tsc[mi] = p.a_scale + (p.row_index ? p.row_index[pos] : pos) * nkb;
+    // scales: a lane loads the one of token row `lane` of the tile, a slab ahead; one (SwiGLU: two) of the weights for the
+    // tile, through the scalar cache
+    uint32_t tso;
+    {
+        const int64_t pos = ti.row0 + std::min(lane % TM, ti.valid - 1);
+        tso = static_cast<uint32_t>(p.row_index ? p.row_index[pos] : pos) * static_cast<uint32_t>(4 * nkb);
     }
     const float* sg = p.b_scale + static_cast<int64_t>(ti.group) * scale_rows(p) * nkb;
-    const float* wsc0 = sg + static_cast<int64_t>(weight_row<TN, SWIGLU>(p, ti.nt, 0) / kFp8Block) * nkb;
-    const float* wsc1 = sg + static_cast<int64_t>(weight_row<TN, SWIGLU>(p, ti.nt, TN / 2) / kFp8Block) * nkb;
+    const cfloat* wsc0 = (const cfloat*)(sg + static_cast<int64_t>(uniform(weight_row<TN, SWIGLU>(p, ti.nt, 0) / kFp8Block)) * nkb);
+    const cfloat* wsc1 =
+        (const cfloat*)(sg + static_cast<int64_t>(uniform(weight_row<TN, SWIGLU>(p, ti.nt, TN / 2) / kFp8Block)) * nkb);
 
     const int soff = (lg ^ swz(l16)) * 16, soff4 = ((4 + lg) ^ swz(l16)) * 16;  // blocks start at multiples of 16 rows
     int foff_t[MI], foff_w[NI];
@@ -253,12 +274,11 @@ __global__ __launch_bounds__(256, 2) void fp8_ring_kernel(Fp8GemmArgs p) {
 #pragma unroll
         for (int mi = 0; mi < MI; ++mi) acc[ni][mi] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    float st_next[MI], sw_next[2];
+    float st_next, sw_next[2];
     auto load_scales = [&](int st) {
-#pragma unroll
-        for (int mi = 0; mi < MI; ++mi) st_next[mi] = tsc[mi][st];
+        st_next = *reinterpret_cast<const float*>(reinterpret_cast<const char*>(p.a_scale + st) + tso);
         sw_next[0] = wsc0[st];
-        sw_next[1] = SWIGLU ? wsc1[st] : sw_next[0];
+        if (SWIGLU) sw_next[1] = wsc1[st];
     };
     auto step = [&](int st, const char* cur, char* refill) {
         if (st >= nkb) return;
@@ -272,11 +292,9 @@ __global__ __launch_bounds__(256, 2) void fp8_ring_kernel(Fp8GemmArgs p) {
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("s_barrier" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
-        float s[NI][MI];
-#pragma unroll
-        for (int ni = 0; ni < NI; ++ni)
-#pragma unroll
-            for (int mi = 0; mi < MI; ++mi) s[ni][mi] = st_next[mi] * sw_next[ni];
+        float s[SWIGLU ? 2 : 1][MI];
+        spread(st_next * sw_next[0], s[0]);
+        if (SWIGLU) spread(st_next * sw_next[1], s[SWIGLU ? 1 : 0]);
         if (st + 1 < nkb) load_scales(st + 1);
         if (st + RING - 1 < nkb) issue(st + RING - 1, refill);
         i32x8 ft[MI], fw[NI];
@@ -290,7 +308,7 @@ __global__ __launch_bounds__(256, 2) void fp8_ring_kernel(Fp8GemmArgs p) {
                            *reinterpret_cast<const uint4*>(cur + foff_t[mi] + soff4));
         auto add = [&](int ni, int mi, f32x4 part) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc[ni][mi][i] = fmaf(part[i], s[ni][mi], acc[ni][mi][i]);
+            for (int i = 0; i < 4; ++i) acc[ni][mi][i] = fmaf(part[i], s[SWIGLU ? ni : 0][mi], acc[ni][mi][i]);
         };
         Wide ww[NI];
 #pragma unroll
@@ -475,19 +493,6 @@ __global__ __launch_bounds__(512, 1) void fp8_pp_kernel(Fp8GemmArgs p) {
         s.w1 = SWIGLU ? ws1[ks] : 0.f;
         return s;
     };
-    // out[mi] of every lane = v of lane 16 mi + l16
-    auto spread = [&](float v, float (&out)[MI]) {
-        typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-        const uint32_t u = __float_as_uint(v);
-        const u32x2 r = __builtin_amdgcn_permlane16_swap(u, u, false, false);    // rows 0 0 2 2, 1 1 3 3
-        const u32x2 e = __builtin_amdgcn_permlane32_swap(r[0], r[0], false, false);  // rows 0 0 0 0, 2 2 2 2
-        const u32x2 o = __builtin_amdgcn_permlane32_swap(r[1], r[1], false, false);
-        out[0] = __uint_as_float(e[0]);
-        out[1] = __uint_as_float(o[0]);
-        out[2] = __uint_as_float(e[1]);
-        out[3] = __uint_as_float(o[1]);
-    };
-
     f32x4 acc[NI][MI];
 #pragma unroll
     for (int ni = 0; ni < NI; ++ni)
