@@ -895,27 +895,33 @@ bool offsets32(const Fp8GemmArgs& a) {
     return (!a.row_index || a.src_rows * a.K < (int64_t(1) << 32)) && a.src_rows * (a.K / kFp8Block) * 4 < (int64_t(1) << 32);
 }
 
-// Rounds of the machine that tiles of tm x tn take, `slots` at a time: full tiles and half of another per group that has
-// rows (the segments' lengths are on the device).
+// Tiles of tm x tn expected of a launch: the segments' lengths are on the device, so a group with rows is taken to have the
+// mean of them and a quarter of a tile more, one tile at least.
+double expected_tiles(const Fp8GemmArgs& a, int tm, int tn) {
+    const double active = static_cast<double>(std::min<int64_t>(a.rows, a.n_groups));
+    const double mt = a.seg ? active * std::max(1.0, a.rows / active / tm + 0.25) : std::ceil(static_cast<double>(a.rows) / tm);
+    return mt * ((a.N + tn - 1) / tn);
+}
 double rounds(const Fp8GemmArgs& a, int tm, int tn, int slots) {
-    const int64_t active = std::min<int64_t>(a.rows, a.n_groups);
-    const int64_t mt = a.seg ? std::max(active, a.rows / tm + active / 2) : (a.rows + tm - 1) / tm;
-    return std::ceil(static_cast<double>(mt * ((a.N + tn - 1) / tn)) / slots);
+    return std::max(1.0, std::ceil(expected_tiles(a, tm, tn) / slots - 0.1));
 }
 
 // Whether the last round of the 256 x 256 tiles may be worth splitting along K: long K, and rounds few enough that it weighs.
 // (Whether it is split, and into how many chunks, follows from the number of tiles, on the device.)
 bool may_split(const Fp8GemmArgs& a, bool swiglu) {
-    return a.K >= 16 * kFp8Block && rounds(a, 256, swiglu ? 128 : 256, 1) <= 8 * kSplitSlots;
+    return a.K >= 16 * kFp8Block && expected_tiles(a, 256, swiglu ? 128 : 256) <= 8 * kSplitSlots;
 }
 
-// The 256 x 256 tiles where their rounds cost less than those of the ring's 64-row ones: a block of K takes about 2.5 us a
-// round (256 tiles, however many of their rows are real: the rate of the weights), 1.9 us a round of the ring's (512).
-// 16 experts, 2048 -> 4096 -> 2048: 133 us with the ring, 155 with them at 32 rows an expert, 173 and 153 at 64, 271 and
-// 160 at 128; 64 experts, 1024 -> 2048 -> 1024: 129 and 158, 191 and 162, 288 and 177.
+// The 256 x 256 tiles where their rounds cost less than those of the ring's 64-row ones. A round of 256 of the former takes
+// about 2 us a block of K and 11 us besides, however many of the rows are real, a round of 512 of the latter 1.55 and 3 us.
+// (16 experts, 2048 -> 4096 -> 2048, the two products with the ring and with the large tiles: 66 + 44 us and 85 + 65 at 48
+// rows an expert, 82 + 53 and 85 + 67 at 64, 101 + 52 and 85 + 66 at 96, 150 + 78 and 84 + 67 at 128; 64 experts, 1024 -> 2048
+// -> 1024: 95 + 53 and 103 + 46 at 64 rows, 119 + 55 and 104 + 46 at 96.)
 bool use_pp(const Fp8GemmArgs& a, bool swiglu) {
-    return offsets32(a) && a.K >= 2 * kFp8Block &&
-           2.5 * rounds(a, 256, swiglu ? 128 : 256, 256) <= 1.9 * rounds(a, 64, swiglu ? 64 : 128, 512);
+    const double nkb = a.K / kFp8Block;
+    return offsets32(a) && nkb >= 2 &&
+           rounds(a, 256, swiglu ? 128 : 256, kSplitSlots) * (2.0 * nkb + 11.0) <=
+               rounds(a, 64, swiglu ? 64 : 128, 512) * (1.55 * nkb + 3.0);
 }
 
 template <typename TO, Epilogue EPI>

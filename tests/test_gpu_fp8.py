@@ -111,7 +111,7 @@ MATMULS = [
     (1200, 2, 514, 768, 9), (64, 256, 32, 128, 0), (2500, 5, 640, 1280, 1), (1111, 4, 1025, 1024, 30),
     # enough 256 x 256 tiles: whole rounds and less, ragged rows and columns, the last round split along K (an even and an
     # odd number of blocks, a chunk without any), widths that no 16-byte store fits
-    (2048, 1, 2176, 384, 0), (2300, 3, 2184, 512, 7), (2300, 3, 2181, 512, 7), (2048, 1, 2176, 2048, 0),
+    (6144, 1, 2176, 384, 0), (5000, 3, 2184, 512, 7), (5000, 3, 2181, 512, 7), (3072, 1, 2304, 2048, 0),
     (2200, 4, 2056, 2176, 100), (8448, 1, 2048, 2176, 0), (16640, 1, 1024, 256, 0),
 ]
 
@@ -236,10 +236,11 @@ def _moe_reference(x, idx, w, w_in, w_down, act, dtype):
     (1500, 2, 1, 2, 384, 256, "swiglu", torch.bfloat16, 0.0),
     (1100, 2, 2, 2, 256, 1152, "swiglu", torch.bfloat16, 0.0),
     # hidden rows quantised by the 256 x 256 tiles, and by the sum over their split last round
-    (2000, 2, 1, 2, 512, 1152, "swiglu", torch.bfloat16, 0.0),
-    (2000, 2, 1, 2, 512, 2432, "relu", torch.bfloat16, 0.5),
-    (1900, 2, 1, 2, 2048, 1152, "swiglu", torch.float32, 0.0),
-    (1900, 2, 1, 2, 2176, 2432, "relu", torch.bfloat16, 0.0),
+    (4200, 2, 1, 2, 512, 1152, "swiglu", torch.bfloat16, 0.0),
+    (4200, 2, 1, 2, 512, 2432, "relu", torch.bfloat16, 0.5),
+    (2600, 2, 1, 2, 2048, 1152, "swiglu", torch.bfloat16, 0.0),
+    (2600, 2, 1, 2, 2048, 1152, "swiglu", torch.float32, 0.0),
+    (2600, 2, 1, 2, 2176, 2432, "relu", torch.bfloat16, 0.0),
 ])
 def test_moe_forward_matches_the_oracle(T, M, k, keep, d, H, act, dtype, skew):
     say(f"fp8_moe_forward T={T} M={M} k={k} d={d} H={H} {act} {dtype}")
