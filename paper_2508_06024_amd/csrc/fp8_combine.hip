@@ -3,7 +3,8 @@
 // The rows come in float32 (few rows an expert, where their traffic is nothing beside the weights') or, from the 256 x
 // 256 tiles, as float16 with a power-of-two scale for each 128 columns of a row: 11 bits in the bytes of bfloat16, whose 8
 // would round every row before the sum (1.2e-3 of the result, beside 1.7e-3 for its own rounding to bfloat16).
-// Accumulated in float32 in slot order and rounded once. One wave per token, 8 columns a lane; few tokens also split
+// Accumulated in float32 in slot order and rounded once; a slot without a row (position -1: its expert id was out of
+// range) adds nothing. One wave per token, 8 columns a lane; few tokens also split
 // the row over blockIdx.y. Memory-bound: 8192 tokens of 2048, 6 slots, 37 us.
 #include "device_common.h"
 #include "fp8.h"
@@ -47,7 +48,7 @@ __global__ __launch_bounds__(64 * kTokens) void fp8_combine_kernel(const void* _
 #pragma unroll
             for (int j = 0; j < KMAX; ++j) {
                 if (MORE && j >= top_k) continue;
-                const int64_t row = pos[j];
+                const int64_t row = std::max(pos[j], 0);
                 if constexpr (HALF) {
                     const uint16_t* src = static_cast<const uint16_t*>(rows) + row * d + c * 8;
                     v[b][j][0] = NT ? ldg16_nt(src) : ldg16(src);
@@ -67,7 +68,7 @@ __global__ __launch_bounds__(64 * kTokens) void fp8_combine_kernel(const void* _
             for (int i = 0; i < 8; ++i) acc[i] = 0.f;
 #pragma unroll
             for (int j = 0; j < KMAX; ++j) {
-                if (MORE && j >= top_k) continue;
+                if ((MORE && j >= top_k) || pos[j] < 0) continue;  // uniform
                 if constexpr (HALF) {
                     const _Float16* h = reinterpret_cast<const _Float16*>(&v[b][j][0]);
                     const float f = wt[j] * s[b][j];  // s a power of two

@@ -303,6 +303,53 @@ def test_moe_forward_on_another_stream_and_captured():
         assert torch.equal(E.fp8_moe_forward(xs[1 - rep % 2], idx, w, *w_in, *w_dn, ws=ws), refs[1 - rep % 2])
 
 
+@pytest.mark.parametrize("T,M,k,d,H,dtype", [
+    (37, 4, 2, 256, 256, torch.bfloat16),
+    (37, 6, 3, 256, 128, torch.float32),
+    (60, 20, 10, 128, 128, torch.bfloat16),   # more slots than the unrolled sums
+    (4200, 2, 2, 1152, 512, torch.bfloat16),  # output rows as float16 with scales
+])
+def test_moe_forward_of_slots_without_an_expert(T, M, k, d, H, dtype):
+    """Ids outside [0, M) add nothing, whatever their weight: as with a weight of zero. K is below the
+    16 blocks from which sums are split, so that a row's bits do not depend on the other rows."""
+    say(f"fp8_moe_forward without experts T={T} M={M} k={k}")
+    rng = np.random.default_rng(T + k)
+    idx = np.stack([rng.permutation(M)[:k] for _ in range(T)]).astype(np.int32)
+    w = rng.random((T, k)).astype(np.float32)
+    off = rng.random((T, k)) < 0.3
+    off[T // 2] = True  # a padding token
+    wild = np.where(rng.random((T, k)) < 0.5, -1, M + rng.integers(0, 1000, (T, k)))
+    x = up(rng.normal(size=(T, d)), dtype)
+    w_in, w_dn = E.fp8_quantize(up(rng.normal(size=(M, 2 * H, d)) * d ** -0.5), 128), E.fp8_quantize(up(rng.normal(size=(M, d, H)) * H ** -0.5), 128)
+    got = E.fp8_moe_forward(x, up(np.where(off, wild, idx), torch.int32), up(w), *w_in, *w_dn)
+    ref = E.fp8_moe_forward(x, up(idx, torch.int32), up(np.where(off, 0, w)), *w_in, *w_dn)
+    assert torch.equal(got, ref) and (got[T // 2] == 0).all() and got.abs().max() > 0
+    none = E.fp8_moe_forward(x, up(wild, torch.int32), up(w), *w_in, *w_dn)
+    assert (none == 0).all()
+
+
+def test_moe_forward_of_two_streams_at_once():
+    """Calls on two streams, each with its own workspace and output, in flight together."""
+    rng = np.random.default_rng(14)
+    M, k, d, H = 8, 2, 512, 512
+    w_in, w_dn = E.fp8_quantize(up(rng.normal(size=(M, 2 * H, d)) * 0.05), 128), E.fp8_quantize(up(rng.normal(size=(M, d, H)) * 0.05), 128)
+    jobs = []
+    for i, T in enumerate((64, 3000)):
+        idx, w = W.gen_routing(T, M, k, list(range(M)), seed=i, skew=0.5)
+        x, idx, w = up(rng.normal(size=(T, d)), torch.bfloat16), up(idx, torch.int32), up(w)
+        desc = E.moe_desc(T, M, 1, d, H, k, torch.bfloat16)
+        jobs.append((desc, x, idx, w, E.fp8_moe_forward(x, idx, w, *w_in, *w_dn), torch.zeros_like(x),
+                     E.workspace(E.fp8_moe_workspace_size(desc), DEV), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for desc, x, idx, w, _, y, ws, stream in jobs:
+            with torch.cuda.stream(stream):
+                E.fp8_moe_forward_into(desc, x, idx, w, *w_in, *w_dn, y, ws)
+    torch.cuda.synchronize()
+    for _, _, _, _, ref, y, _, _ in jobs:
+        assert torch.equal(y, ref)
+
+
 def test_layer_with_8_bit_experts():
     """Ec2moeLayer: routing, codec and reconstruction as with bfloat16 experts, the experts' output that
     of fp8_moe_forward on them."""
