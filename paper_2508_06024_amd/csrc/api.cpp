@@ -545,6 +545,15 @@ ec2moe_status ec2moe_fp8_quantize(const void* x, ec2moe_dtype x_dtype, int32_t n
 
 namespace {
 
+constexpr const char* kFp8MatmulName = "fp8_matmul";  // of the timing record; outside the layer step
+
+Fp8GemmArgs fp8_matmul_shape(const ec2moe_fp8_matmul_desc* d, const int32_t* seg) {
+    Fp8GemmArgs g{};
+    g.seg = seg; g.n_groups = d->n_groups; g.rows = d->rows; g.src_rows = d->rows; g.b_rows = d->n; g.K = d->k; g.N = d->n;
+    g.name = kFp8MatmulName;
+    return g;
+}
+
 ec2moe_status check_fp8_desc(const ec2moe_fp8_matmul_desc* d) {
     REQUIRE(d != nullptr, EC2MOE_ERR_INVALID_ARGUMENT, "desc is NULL");
     REQUIRE(d->out_dtype == EC2MOE_F32 || d->out_dtype == EC2MOE_BF16, EC2MOE_ERR_INVALID_ARGUMENT, "unknown dtype %d",
@@ -555,18 +564,10 @@ ec2moe_status check_fp8_desc(const ec2moe_fp8_matmul_desc* d) {
     REQUIRE(d->k % kFp8Block == 0, EC2MOE_ERR_UNSUPPORTED, "k %d is not a multiple of %d", d->k, kFp8Block);
     REQUIRE(static_cast<int64_t>(d->n) * d->k < (int64_t(1) << 32), EC2MOE_ERR_UNSUPPORTED,
             "a weight matrix of %d x %d is too large for 32-bit byte offsets", d->n, d->k);
-    REQUIRE(fp8_gemm_fits(d->rows, d->n_groups, d->n), EC2MOE_ERR_UNSUPPORTED, "%d x %d outputs are too many for one launch",
-            d->rows, d->n);
+    const int32_t some = 0;
+    REQUIRE(fp8_gemm_fits(fp8_matmul_shape(d, &some)), EC2MOE_ERR_UNSUPPORTED,
+            "a product of %d x %d x %d is too large for one launch", d->rows, d->n, d->k);
     return EC2MOE_OK;
-}
-
-constexpr const char* kFp8MatmulName = "fp8_matmul";  // of the timing record; outside the layer step
-
-Fp8GemmArgs fp8_matmul_shape(const ec2moe_fp8_matmul_desc* d, const int32_t* seg) {
-    Fp8GemmArgs g{};
-    g.seg = seg; g.n_groups = d->n_groups; g.rows = d->rows; g.src_rows = d->rows; g.b_rows = d->n; g.K = d->k; g.N = d->n;
-    g.name = kFp8MatmulName;
-    return g;
 }
 
 // (float32 outputs take no split; either way of giving the segments may)
@@ -679,15 +680,15 @@ ec2moe_status ec2moe_fp8_moe_forward(const ec2moe_moe_desc* desc, const void* x,
     const DType dt = static_cast<DType>(desc->dtype);
     const int T = desc->n_tokens, d = desc->d_model, H = desc->ffn_hidden, M = desc->n_experts;
     const int64_t A = static_cast<int64_t>(T) * desc->top_k;
-    REQUIRE(fp8_gemm_fits(A, M, H) && fp8_gemm_fits(A, M, d), EC2MOE_ERR_UNSUPPORTED,
-            "%lld assignments are too many for one launch", static_cast<long long>(A));
     int32_t* seg = at<int32_t>(ws, w.seg);
     int32_t* perm_src = at<int32_t>(ws, w.perm_src);
     int32_t* inv_perm = at<int32_t>(ws, w.inv_perm);
+    Fp8Experts x8 = fp8_experts(desc, seg, perm_src);
+    REQUIRE(fp8_gemm_fits(x8.in) && fp8_gemm_fits(x8.out), EC2MOE_ERR_UNSUPPORTED,
+            "%lld assignments are too many for one launch", static_cast<long long>(A));
     hipError_t e = launch_permute(topk_idx, A, desc->top_k, M, at<int32_t>(ws, w.counts), seg, perm_src, inv_perm,
                                   stream);
     if (e == hipSuccess) e = launch_fp8_quantize(dt, x, 1, T, d, 1, at<void>(ws, w.xq), at<float>(ws, w.xs), stream);
-    Fp8Experts x8 = fp8_experts(desc, seg, perm_src);
     if (e == hipSuccess) {
         Fp8GemmArgs& g = x8.in;
         g.a = at<uint8_t>(ws, w.xq); g.a_scale = at<float>(ws, w.xs); g.b = static_cast<const uint8_t*>(w_gate_up);

@@ -934,14 +934,11 @@ hipError_t dispatch_small(const Fp8GemmArgs& a, hipStream_t s) {
 
 }  // namespace
 
-bool fp8_gemm_fits(int64_t rows, int n_groups, int64_t n) {
-    Fp8GemmArgs a{};
-    a.rows = rows;
-    a.n_groups = n_groups;
-    a.N = static_cast<int>(n);
-    int seg = 0;
-    a.seg = &seg;
-    return max_tiles(a, 16, 32) < (int64_t(1) << 23);  // workgroups of 256 threads of a launch: 2^32 threads at most
+bool fp8_gemm_fits(const Fp8GemmArgs& a) {
+    // a launch holds fewer than 2^32 threads: 512 a tile of the few-row kernel, 256 a tile of the ring (32 x 64 at least)
+    if (max_tiles(a, 32, 64) >= (int64_t(1) << 24) - kXcds || (!offsets32(a) && max_tiles(a, 16, 16) >= (int64_t(1) << 23) - kXcds))
+        return false;
+    return a.K < 1 << 24;  // 32-bit byte offsets of the 256 rows of a tile
 }
 
 hipError_t launch_fp8_gemm(DType out_type, const Fp8GemmArgs& a, hipStream_t s) {

@@ -42,6 +42,16 @@ def test_matmul(kw, status):
     assert _mm(**kw) == status, E.last_error()
 
 
+def test_matmul_sizes_one_launch_can_hold():
+    """Fewer than 2^32 threads over the tiles, 32-bit offsets within a tile: refused beyond, not at, the largest."""
+    ok = lambda rows, n, k: E._lib.ec2moe_fp8_matmul_workspace_size(ctypes.byref(E.Fp8MatmulDesc(rows, 1, n, k, E.BF16)),
+                                                                    ctypes.byref(ctypes.c_size_t(0)))
+    assert ok(2 ** 18, 2 ** 16, 4096) == OK and ok(2 ** 20, 2 ** 14, 128) == OK
+    assert ok(2 ** 19, 2 ** 17, 4096) == UNSUPPORTED and ok(2 ** 31 - 1, 2 ** 10, 128) == UNSUPPORTED
+    assert ok(1, 1, 2 ** 24 - 128) == OK and ok(1, 1, 2 ** 24) == UNSUPPORTED
+    assert ok(2 ** 31 - 1, 1, 2 ** 23) == UNSUPPORTED  # 2^54 bytes of rows: the few-row kernel's tiles
+
+
 def _desc(**kw):
     base = dict(n_tokens=64, n_experts=8, n_groups=2, d_model=128, ffn_hidden=256, top_k=2, dtype=E.BF16, renormalize=True)
     base.update(kw)
