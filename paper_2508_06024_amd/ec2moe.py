@@ -553,10 +553,10 @@ def group_gate_backward_into(desc: MoeDesc, opts: Optional[GateOpts], x, w_globa
 
 
 def group_gate_backward(x, w_global, w_local, probs, topk_idx, d_topk_w=None, d_probs=None, d_balance=None,
-                        token_valid=None, renormalize=True, group_sizes=None, with_dx=True, ws=None):
+                        token_valid=None, renormalize=True, group_sizes=None, with_dx=True, ws=None, top_groups=0):
     """Gradients (d_x, d_w_global, d_b_global, d_w_local, d_b_local) of the gate's inputs from those of
     its outputs: d_topk_w [T][k], d_probs [T][M], and d_balance [M], which every valid token shares.
-    The gate must have kept every group (top_groups 0). d_x (None without with_dx) has x's type, the
+    top_groups as given to the gate, which must have kept every group (else refused). d_x (None without with_dx) has x's type, the
     others are float32."""
     T, d = x.shape
     M, K = w_local.shape[0], w_global.shape[0]
@@ -575,7 +575,7 @@ def group_gate_backward(x, w_global, w_local, probs, topk_idx, d_topk_w=None, d_
     new = lambda *shape: torch.empty(shape, dtype=torch.float32, device=x.device)
     d_x = torch.empty_like(x) if with_dx else None
     d_wg, d_bg, d_wl, d_bl = new(K, d), new(K), new(M, d), new(M)
-    group_gate_backward_into(desc, gate_opts(0, group_sizes), x, w_global, w_local, probs, topk_idx, ws, d_topk_w, d_probs,
+    group_gate_backward_into(desc, gate_opts(top_groups, group_sizes), x, w_global, w_local, probs, topk_idx, ws, d_topk_w, d_probs,
                              d_balance, _valid_bytes(token_valid, T), d_x, d_wg, d_bg, d_wl, d_bl)
     return d_x, d_wg, d_bg, d_wl, d_bl
 

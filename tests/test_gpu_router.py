@@ -162,6 +162,45 @@ def test_gate_backward_matches_the_oracle(T, d, M, K, k, keep, uneven, renorm, t
     assert no_dx[0] is None and all(torch.equal(a, b) for a, b in zip(got[1:], no_dx[1:]))
 
 
+@pytest.mark.parametrize("renorm", [True, False])
+def test_gate_backward_of_repeated_and_missing_selections(renorm):
+    """A token may name an expert twice (its gradients add), and an id outside [0, M) selects nothing."""
+    rng = np.random.default_rng(15)
+    T, d, M, K, k = 70, 128, 16, 4, 4
+    g = _probs(rng, T, M, set(range(M)), [4] * 4)
+    idx = _topk(g, k)
+    idx[:, 3] = idx[:, 0]
+    dw = rng.normal(size=(T, k)).astype(np.float32)
+    x, wg, wl = (up(rng.normal(size=(n, d)) * 0.3) for n in (T, K, M))
+    groups = [list(range(4 * i, 4 * i + 4)) for i in range(K)]
+    X, WG, WL = down(x), down(wg), down(wl)
+
+    def check(got, sel, dw):
+        dl, du, al, au = (np.zeros((T, n)) for n in (M, K, M, K))
+        for t in range(T):  # the oracle takes selections of one length
+            keep = (sel[t] >= 0) & (sel[t] < M)
+            o = OO.gate_backward(g[t:t + 1].astype(np.float64), sel[t:t + 1, keep], groups, renorm, dw[t:t + 1, keep])
+            dl[t], du[t], al[t], au[t] = (a[0] for a in o)
+        e0 = (M + k + 24) * 2.0 ** -24
+        eX, eT = e0 + (M + K + 1) * 2.0 ** -24, e0 + (T + 16) * 2.0 ** -24
+        _check("d_x", down(got[0]), dl @ WL + du @ WG, eX * (al @ np.abs(WL) + au @ np.abs(WG)) + 1e-37)
+        _check("d_w_global", down(got[1]), du.T @ X, eT * (au.T @ np.abs(X)) + 1e-37)
+        _check("d_w_local", down(got[3]), dl.T @ X, eT * (al.T @ np.abs(X)) + 1e-37)
+
+    call = lambda sel: E.group_gate_backward(x, wg, wl, up(g), up(sel, torch.int32), up(dw), renormalize=renorm)
+    check(call(idx), idx, dw)
+    idx[:, 1] = np.where(np.arange(T) % 2, -1, M + 5)
+    check(call(idx), idx, dw)
+
+
+def test_gate_backward_refuses_pruned_groups():
+    x, wg, wl = (torch.zeros((n, 128), device=DEV) for n in (4, 2, 8))
+    g, idx = torch.full((4, 8), 0.125, device=DEV), torch.zeros((4, 2), dtype=torch.int32, device=DEV)
+    with pytest.raises(E.Ec2moeError):
+        E.group_gate_backward(x, wg, wl, g, idx, top_groups=1)
+    assert E.group_gate_backward(x, wg, wl, g, idx, top_groups=2)[0].abs().sum() == 0
+
+
 def test_gate_backward_of_one_renormalised_selection_is_zero():
     rng = np.random.default_rng(4)
     g = _probs(rng, 50, 8, set(range(8)), [4, 4])
