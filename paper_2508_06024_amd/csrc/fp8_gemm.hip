@@ -9,10 +9,17 @@
 //
 // Three kernels:
 //   * fp8_skinny_kernel (few rows a group): a stream of the weights, straight from memory to registers;
-//   * fp8_ring_kernel (64-row tiles): operands through a ring of LDS slabs;
-//   * fp8_pp_kernel (256 x 256 tiles): two groups of waves that alternate between products and memory.
-// The first two multiply exactly, through bfloat16, for float32 outputs (and the first always: a stream of
-// weights leaves the matrix cores idle); the others use the 8-bit matrix core, at twice the rate.
+//   * fp8_ring_kernel (32- and 64-row tiles): operands through a ring of LDS slabs;
+//   * fp8_pp_kernel (256 x 256 tiles, bfloat16 outputs and hidden rows): two groups of waves that alternate between
+//     products and memory.
+// The first two multiply exactly, through bfloat16 (at one row to some tens a group, memory bounds them; float32 outputs
+// ask for it); the last uses the 8-bit matrix core, at twice the rate, whose sums are cut off as fp8_device.h says.
+//
+// Measured: one row of 4096 x 4096 weights 5.8 us (2.9 TB/s of weights, a launch's length); 32 tokens through 40 of 64
+// experts of 4096 -> 1536, 8 a token, 86 us (5.8 TB/s) and 50 (5.0); 8 experts of 4096 -> 14336, 8192 rows, 2.05
+// PFLOP/s in and 2.0 out, the chip at its power limit (1.64 GHz under the gate-up product); 49152 rows over 48 experts of
+// 2048 -> 1408, 1.6 and 1.4 PFLOP/s: 5 to 9 us of every 16 or 11 slabs' round go into the tile's end, whose stores all
+// workgroups make at once.
 #include "device_common.h"
 #include "fp8_device.h"
 #include "gemm_tiles.h"
@@ -190,12 +197,14 @@ __device__ __forceinline__ int weight_row(const Fp8GemmArgs& p, int nt, int n) {
     return std::min(nt * TN + n, p.b_rows - 1);
 }
 
-// ------------------------------------------------------------------ 64-row tiles through a ring
+// ------------------------------------------------------------------ 32- and 64-row tiles through a ring
 //
 // Tiles of TM x 128 over the whole K: slabs of one block of 128 (128-byte pieces of each row) go through
 // a ring of RING LDS stages filled by buffer_load ... lds, RING - 1 of them in flight behind counted waits
 // and one barrier per slab. Four waves of TM x 32. Chunk c of staged row R sits at c ^ ((R >> 1) & 7).
 // STREAM: the weights pass the caches by (each is read once).
+// Bound by the vector instructions: 96 conversions and 128 multiply-adds a wave a slab beside its 32 products (3000 rows in 12
+// segments, 2048 -> 2001, float32: 52 us, 0.47 PFLOP/s), or by the weights' stream.
 template <typename TO, int TM, int RING, Epilogue EPI, bool STREAM>
 __global__ __launch_bounds__(256, 2) void fp8_ring_kernel(Fp8GemmArgs p) {
     constexpr bool SWIGLU = EPI == Epilogue::SwiGLU;
@@ -373,9 +382,9 @@ __global__ __launch_bounds__(256, 2) void fp8_ring_kernel(Fp8GemmArgs p) {
 // block's 32 bytes a lane are read AHEAD blocks of products ahead, behind the same barriers. Scales are loaded a slab
 // ahead and before the slab loads of the phase, so that its counted waits cover them. The 128
 // scaling multiply-adds of a slab issue under its products (16 of every 32 cycles).
-// EPI Store writes bfloat16 rows, or (HALF) float16 rows with a power-of-two scale for each 128 columns, a wave's. SwiGLU and ReLU quantise: a tile holds one (ReLU: two) whole blocks of 128
-// hidden columns of each row, whose largest value meets across the lanes and, with SwiGLU, the two
-// waves of the row.
+// EPI Store writes bfloat16 rows, or (HALF) float16 rows with a power-of-two scale for each 128 columns, a wave's. SwiGLU
+// and ReLU quantise: a tile holds one (ReLU: two) whole blocks of 128 hidden columns of each row, whose largest value
+// meets across the lanes and, with SwiGLU, the two waves of the row.
 template <Epilogue EPI, bool HALF = false>
 __global__ __launch_bounds__(512, 1) void fp8_pp_kernel(Fp8GemmArgs p) {
     constexpr bool SWIGLU = EPI == Epilogue::SwiGLU;
