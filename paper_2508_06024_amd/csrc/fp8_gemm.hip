@@ -9,7 +9,7 @@
 //
 // Three kernels:
 //   * fp8_skinny_kernel (few rows a group): a stream of the weights, straight from memory to registers;
-//   * fp8_ring_kernel (32- and 64-row tiles): operands through a ring of LDS slabs;
+//   * fp8_ring_kernel (32- to 128-row tiles): operands through a ring of LDS slabs;
 //   * fp8_pp_kernel (256 x 256 tiles, bfloat16 outputs and hidden rows): two groups of waves that alternate between
 //     products and memory.
 // The first two multiply exactly, through bfloat16 (at one row to some tens a group, memory bounds them; float32 outputs
@@ -197,27 +197,30 @@ __device__ __forceinline__ int weight_row(const Fp8GemmArgs& p, int nt, int n) {
     return std::min(nt * TN + n, p.b_rows - 1);
 }
 
-// ------------------------------------------------------------------ 32- and 64-row tiles through a ring
+// ------------------------------------------------------------------ 32- to 128-row tiles through a ring
 //
 // Tiles of TM x 128 over the whole K: slabs of one block of 128 (128-byte pieces of each row) go through
 // a ring of RING LDS stages filled by buffer_load ... lds, RING - 1 of them in flight behind counted waits
-// and one barrier per slab. Four waves of TM x 32. Chunk c of staged row R sits at c ^ ((R >> 1) & 7).
+// and one barrier per slab. Four waves of TM x 32, or of 64 x 64 of 128 rows. Chunk c of staged row R sits at c ^ ((R >> 1) & 7).
 // STREAM: the weights pass the caches by (each is read once).
-// Bound by the vector instructions: 96 conversions and 128 multiply-adds a wave a slab beside its 32 products (3000 rows in 12
-// segments, 2048 -> 2001, float32: 52 us, 0.47 PFLOP/s), or by the weights' stream.
+// Bound by the conversions to bfloat16 (96 a wave a slab for 32 products at 64 rows, 128 for 64 at 128; about as long as a
+// product each), or by the weights' stream. 3000 rows in 12 segments, 2048 -> 2001, float32: 52 us with 64 rows, 45 with
+// 128 (0.54 PFLOP/s).
 template <typename TO, int TM, int RING, Epilogue EPI, bool STREAM>
 __global__ __launch_bounds__(256, 2) void fp8_ring_kernel(Fp8GemmArgs p) {
     constexpr bool SWIGLU = EPI == Epilogue::SwiGLU;
     constexpr int TN = 128;
     constexpr int NLD = (TM + TN) / 32;  // load instructions (8 rows) per wave per slab
-    constexpr int MI = TM / 16, NI = 2;
+    constexpr int WM = TM > 64 ? 2 : 1, WN = 4 / WM;  // waves
+    constexpr int MI = TM / WM / 16, NI = TN / WN / 16;
+    constexpr int NBK = SWIGLU ? NI / 2 : NI;  // blocks of 16 output columns of a wave
     constexpr int NOUT = SWIGLU ? TN / 2 : TN;
     constexpr int STAGE = (TM + TN) * kFp8Block;
     static_assert((TM + TN) % 32 == 0 && TM % 16 == 0, "whole load instructions");
-    static_assert(RING == 3 || RING == 4, "ring of 3 or 4 slabs");
+    static_assert(RING >= 2 && RING <= 4, "ring of 2 to 4 slabs");
     __shared__ __attribute__((aligned(1024))) char lds0[STAGE];
     __shared__ __attribute__((aligned(1024))) char lds1[STAGE];
-    __shared__ __attribute__((aligned(1024))) char lds2[STAGE];
+    __shared__ __attribute__((aligned(1024))) char lds2[RING > 2 ? STAGE : 16];
     __shared__ __attribute__((aligned(1024))) char lds3[RING > 3 ? STAGE : 16];
 
     const int ntn = (p.N + NOUT - 1) / NOUT;
@@ -227,6 +230,7 @@ __global__ __launch_bounds__(256, 2) void fp8_ring_kernel(Fp8GemmArgs p) {
     asm volatile("" : "+v"(tid));
     const int lane = tid & 63, wave = uniform(tid >> 6);
     const int l16 = lane & 15, lg = lane >> 4;
+    const int wm = wave % WM, wn = wave / WM;
     const int K = p.K, nkb = K / kFp8Block;
 
     auto swz = [](int R) { return (R >> 1) & 7; };
@@ -262,7 +266,7 @@ __global__ __launch_bounds__(256, 2) void fp8_ring_kernel(Fp8GemmArgs p) {
     // tile, through the scalar cache
     uint32_t tso;
     {
-        const int64_t pos = ti.row0 + std::min(lane % TM, ti.valid - 1);
+        const int64_t pos = ti.row0 + std::min(wm * (TM / WM) + lane % (TM / WM), ti.valid - 1);
         tso = static_cast<uint32_t>(p.row_index ? p.row_index[pos] : pos) * static_cast<uint32_t>(4 * nkb);
     }
     const float* sg = p.b_scale + static_cast<int64_t>(ti.group) * scale_rows(p) * nkb;
@@ -273,10 +277,10 @@ __global__ __launch_bounds__(256, 2) void fp8_ring_kernel(Fp8GemmArgs p) {
     const int soff = (lg ^ swz(l16)) * 16, soff4 = ((4 + lg) ^ swz(l16)) * 16;  // blocks start at multiples of 16 rows
     int foff_t[MI], foff_w[NI];
 #pragma unroll
-    for (int mi = 0; mi < MI; ++mi) foff_t[mi] = (mi * 16 + l16) * kFp8Block;
+    for (int mi = 0; mi < MI; ++mi) foff_t[mi] = (wm * (TM / WM) + mi * 16 + l16) * kFp8Block;
 #pragma unroll
     for (int ni = 0; ni < NI; ++ni)
-        foff_w[ni] = (TM + (SWIGLU ? ni * (TN / 2) + wave * 16 : wave * 32 + ni * 16) + l16) * kFp8Block;
+        foff_w[ni] = (TM + (SWIGLU ? ni / NBK * (TN / 2) : 0) + (wn * NBK + ni % NBK) * 16 + l16) * kFp8Block;
     f32x4 acc[NI][MI];
 #pragma unroll
     for (int ni = 0; ni < NI; ++ni)
@@ -293,8 +297,8 @@ __global__ __launch_bounds__(256, 2) void fp8_ring_kernel(Fp8GemmArgs p) {
         if (st >= nkb) return;
         // slabs issued after this one stay in flight
         const int later = std::min(RING - 2, nkb - 1 - st);
-        if (RING == 4 && later >= 2) __builtin_amdgcn_s_waitcnt(vmcnt_imm(2 * NLD));
-        else if (later >= 1) __builtin_amdgcn_s_waitcnt(vmcnt_imm(NLD));
+        if (RING > 3 && later >= 2) __builtin_amdgcn_s_waitcnt(vmcnt_imm(2 * NLD));
+        else if (RING > 2 && later >= 1) __builtin_amdgcn_s_waitcnt(vmcnt_imm(NLD));
         else __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
         // every wave's loads of this slab have landed, and every wave is done with the previous
         // slab, whose slot is refilled next
@@ -317,24 +321,39 @@ __global__ __launch_bounds__(256, 2) void fp8_ring_kernel(Fp8GemmArgs p) {
                            *reinterpret_cast<const uint4*>(cur + foff_t[mi] + soff4));
         auto add = [&](int ni, int mi, f32x4 part) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc[ni][mi][i] = fmaf(part[i], s[SWIGLU ? ni : 0][mi], acc[ni][mi][i]);
+            for (int i = 0; i < 4; ++i) acc[ni][mi][i] = fmaf(part[i], s[ni / NBK][mi], acc[ni][mi][i]);
         };
         Wide ww[NI];
 #pragma unroll
         for (int ni = 0; ni < NI; ++ni) ww[ni] = widen(fw[ni]);
+        // the products of a token block in NI chains side by side, then the multiply-adds of the block before
+        f32x4 part[2][NI];
 #pragma unroll
-        for (int mi = 0; mi < MI; ++mi) {
-            const Wide wt = widen(ft[mi]);
+        for (int mi = 0; mi <= MI; ++mi) {
+            if (mi < MI) {
+                const Wide wt = widen(ft[mi < MI ? mi : 0]);
 #pragma unroll
-            for (int ni = 0; ni < NI; ++ni) add(ni, mi, mfma_wide(ww[ni], wt));
+                for (int ni = 0; ni < NI; ++ni) part[mi & 1][ni] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int ni = 0; ni < NI; ++ni)
+                        part[mi & 1][ni] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ww[ni].v[i], wt.v[i], part[mi & 1][ni], 0, 0, 0);
+            }
+            if (mi > 0)
+#pragma unroll
+                for (int ni = 0; ni < NI; ++ni) add(ni, mi - 1, part[(mi - 1) & 1][ni]);
         }
     };
     load_scales(0);
     issue(0, lds0);
-    if (nkb > 1) issue(1, lds1);
-    if (RING == 4 && nkb > 2) issue(2, lds2);
+    if (RING > 2 && nkb > 1) issue(1, lds1);
+    if (RING > 3 && nkb > 2) issue(2, lds2);
     for (int st = 0; st < nkb; st += RING) {
-        if constexpr (RING == 3) {
+        if constexpr (RING == 2) {
+            step(st, lds0, lds1);
+            step(st + 1, lds1, lds0);
+        } else if constexpr (RING == 3) {
             step(st, lds0, lds2);
             step(st + 1, lds1, lds0);
             step(st + 2, lds2, lds1);
@@ -349,16 +368,16 @@ __global__ __launch_bounds__(256, 2) void fp8_ring_kernel(Fp8GemmArgs p) {
     const bool runs = p.N % 4 == 0;
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) {
-        const int r = mi * 16 + l16;
+        const int r = wm * (TM / WM) + mi * 16 + l16;
         if (r >= ti.valid) continue;
         TO* orow = out + (ti.row0 + r) * p.N;
 #pragma unroll
-        for (int ni = 0; ni < (SWIGLU ? 1 : NI); ++ni) {
-            const int c = ti.nt * NOUT + (SWIGLU ? wave * 16 : wave * 32 + ni * 16) + 4 * lg;
+        for (int ni = 0; ni < NBK; ++ni) {
+            const int c = ti.nt * NOUT + (wn * NBK + ni) * 16 + 4 * lg;
             f32x4 v = acc[ni][mi];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (SWIGLU) v[i] = silu(v[i]) * acc[NI - 1][mi][i];
+                if (SWIGLU) v[i] = silu(v[i]) * acc[SWIGLU ? ni + NBK : ni][mi][i];
                 else if (EPI == Epilogue::ReLU) v[i] = relu(v[i]);
             }
             if (c < p.N) store_run(orow + c, v, p.N - c, c + 4 <= p.N && runs);
@@ -933,11 +952,23 @@ bool use_pp(const Fp8GemmArgs& a, bool swiglu) {
                rounds(a, 64, swiglu ? 64 : 128, 512) * (1.55 * nkb + 3.0);
 }
 
+// Time of the ring's tiles of tm rows (us): two workgroups a CU, each of tm x 128 products, take 1.35 (64 rows) or 2.25 us
+// (128) a block of K together and 0.9 or 1.25 alone, and 3 us besides. The larger tile makes half the conversions a product and
+// wins from two rounds of the smaller on. Measured, 64 and 128 rows (float32 outputs): one matrix 4096 x 4096 with 512
+// rows 33 and 42, 1024 rows 45 and 45, 4096 rows 159 and 129; 8 groups 2048 -> 2048 of 100 rows 19 and 24, 200 rows 25 and 25, 400
+// rows 44 and 36; 64 groups 2048 -> 1408 of 32 rows 38 and 50, 100 rows 66 and 55, 128 rows 75 and 81, 500 rows 261 and 222.
+double ring_cost(const Fp8GemmArgs& a, int tm, int tn) {
+    const double nkb = a.K / kFp8Block;
+    const int halves = std::max(1, static_cast<int>(std::ceil(expected_tiles(a, tm, tn) / 256 - 0.1)));
+    return halves / 2 * ((tm == 64 ? 1.35 : 2.25) * nkb + 3.0) + halves % 2 * ((tm == 64 ? 0.9 : 1.25) * nkb + 3.0);
+}
+
 template <typename TO, Epilogue EPI>
 hipError_t dispatch_small(const Fp8GemmArgs& a, hipStream_t s) {
     const int tn = EPI == Epilogue::SwiGLU ? 64 : 128;
     if (!offsets32(a) || (avg_rows(a) < 32 && max_tiles(a, 32, tn) < 512)) return run_skinny<TO, 1, 1, 8, 4, EPI>(a, s);
     if (avg_rows(a) < 16) return run_ring<TO, 32, 4, EPI, true>(a, s);
+    if (ring_cost(a, 128, tn) < ring_cost(a, 64, tn)) return run_ring<TO, 128, 2, EPI, false>(a, s);
     return run_ring<TO, 64, 3, EPI, false>(a, s);
 }
 

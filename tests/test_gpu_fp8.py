@@ -111,7 +111,7 @@ MATMULS = [
     (1200, 2, 514, 768, 9), (64, 256, 32, 128, 0), (2500, 5, 640, 1280, 1), (1111, 4, 1025, 1024, 30),
     # enough 256 x 256 tiles: whole rounds and less, ragged rows and columns, the last round split along K (an even and an
     # odd number of blocks, a chunk without any), widths that no 16-byte store fits
-    (6144, 1, 2176, 384, 0), (5000, 3, 2184, 512, 7), (5000, 3, 2181, 512, 7), (3072, 1, 2304, 2048, 0),
+    (6144, 1, 2176, 384, 0), (5000, 3, 2184, 512, 7), (5000, 3, 2181, 512, 7), (3328, 1, 2304, 2048, 0),
     (2200, 4, 2056, 2176, 100), (8448, 1, 2048, 2176, 0), (16640, 1, 1024, 256, 0),
 ]
 
