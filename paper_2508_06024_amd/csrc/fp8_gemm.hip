@@ -12,8 +12,8 @@
 //   * fp8_ring_kernel (32- to 128-row tiles): operands through a ring of LDS slabs;
 //   * fp8_pp_kernel (256 x 256 tiles, bfloat16 outputs and hidden rows): two groups of waves that alternate between
 //     products and memory.
-// The first two multiply exactly, through bfloat16 (at one row to some tens a group, memory bounds them; float32 outputs
-// ask for it); the last uses the 8-bit matrix core, at twice the rate, whose sums are cut off as fp8_device.h says.
+// The first, the ring's 32-row tiles and float32 outputs multiply exactly, through bfloat16 (with few rows a group memory is
+// the bound); the others use the 8-bit matrix core, at twice the rate, whose sums are cut off as fp8_device.h says.
 //
 // Measured: one row of 4096 x 4096 weights 5.8 us (2.9 TB/s of weights, a launch's length); 32 tokens through 40 of 64
 // experts of 4096 -> 1536, 8 a token, 86 us (5.8 TB/s) and 50 (5.0); 8 experts of 4096 -> 14336, 8192 rows, 2.05
@@ -203,10 +203,10 @@ __device__ __forceinline__ int weight_row(const Fp8GemmArgs& p, int nt, int n) {
 // a ring of RING LDS stages filled by buffer_load ... lds, RING - 1 of them in flight behind counted waits
 // and one barrier per slab. Four waves of TM x 32, or of 64 x 64 of 128 rows. Chunk c of staged row R sits at c ^ ((R >> 1) & 7).
 // STREAM: the weights pass the caches by (each is read once).
-// Bound by the conversions to bfloat16 (96 a wave a slab for 32 products at 64 rows, 128 for 64 at 128; about as long as a
-// product each), or by the weights' stream. 3000 rows in 12 segments, 2048 -> 2001, float32: 52 us with 64 rows, 45 with
-// 128 (0.54 PFLOP/s).
-template <typename TO, int TM, int RING, Epilogue EPI, bool STREAM>
+// EXACT: products through bfloat16, bound by the conversions (96 a wave a slab for 32 products at 64 rows, 128 for 64 at 128;
+// about as long as a product each): 3000 rows in 12 segments, 2048 -> 2001, float32: 52 us with 64 rows, 45 with 128 (0.54
+// PFLOP/s). Else the 8-bit core: 8 groups of 400 rows, 2048 -> 2048, 25 us (1.1 PFLOP/s).
+template <typename TO, int TM, int RING, Epilogue EPI, bool STREAM, bool EXACT>
 __global__ __launch_bounds__(256, 2) void fp8_ring_kernel(Fp8GemmArgs p) {
     constexpr bool SWIGLU = EPI == Epilogue::SwiGLU;
     constexpr int TN = 128;
@@ -323,22 +323,29 @@ __global__ __launch_bounds__(256, 2) void fp8_ring_kernel(Fp8GemmArgs p) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[ni][mi][i] = fmaf(part[i], s[ni / NBK][mi], acc[ni][mi][i]);
         };
-        Wide ww[NI];
-#pragma unroll
-        for (int ni = 0; ni < NI; ++ni) ww[ni] = widen(fw[ni]);
         // the products of a token block in NI chains side by side, then the multiply-adds of the block before
+        Wide ww[NI];
+        if constexpr (EXACT)
+#pragma unroll
+            for (int ni = 0; ni < NI; ++ni) ww[ni] = widen(fw[ni]);
         f32x4 part[2][NI];
 #pragma unroll
         for (int mi = 0; mi <= MI; ++mi) {
             if (mi < MI) {
-                const Wide wt = widen(ft[mi < MI ? mi : 0]);
+                const i32x8 t = ft[mi < MI ? mi : 0];
+                if constexpr (EXACT) {
+                    const Wide wt = widen(t);
 #pragma unroll
-                for (int ni = 0; ni < NI; ++ni) part[mi & 1][ni] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    for (int ni = 0; ni < NI; ++ni) part[mi & 1][ni] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                    for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int ni = 0; ni < NI; ++ni)
-                        part[mi & 1][ni] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ww[ni].v[i], wt.v[i], part[mi & 1][ni], 0, 0, 0);
+                        for (int ni = 0; ni < NI; ++ni)
+                            part[mi & 1][ni] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ww[ni].v[i], wt.v[i], part[mi & 1][ni], 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int ni = 0; ni < NI; ++ni) part[mi & 1][ni] = mfma8(fw[ni], t);
+                }
             }
             if (mi > 0)
 #pragma unroll
@@ -893,10 +900,10 @@ hipError_t run_skinny(const Fp8GemmArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
-template <typename TO, int TM, int RING, Epilogue EPI, bool STREAM>
+template <typename TO, int TM, int RING, Epilogue EPI, bool STREAM, bool EXACT>
 hipError_t run_ring(const Fp8GemmArgs& a, hipStream_t s) {
     ProfileScope prof(a.name, s);
-    hipLaunchKernelGGL((fp8_ring_kernel<TO, TM, RING, EPI, STREAM>), dim3(tile_grid(a, TM, EPI == Epilogue::SwiGLU ? 64 : 128)),
+    hipLaunchKernelGGL((fp8_ring_kernel<TO, TM, RING, EPI, STREAM, EXACT>), dim3(tile_grid(a, TM, EPI == Epilogue::SwiGLU ? 64 : 128)),
                        dim3(256), 0, s, a);
     return hipGetLastError();
 }
@@ -930,46 +937,66 @@ double expected_tiles(const Fp8GemmArgs& a, int tm, int tn) {
     const double mt = a.seg ? active * std::max(1.0, a.rows / active / tm + 0.25) : std::ceil(static_cast<double>(a.rows) / tm);
     return mt * ((a.N + tn - 1) / tn);
 }
-double rounds(const Fp8GemmArgs& a, int tm, int tn, int slots) {
-    return std::max(1.0, std::ceil(expected_tiles(a, tm, tn) / slots - 0.1));
-}
-
 // Whether the last round of the 256 x 256 tiles may be worth splitting along K: long K, and rounds few enough that it weighs.
 // (Whether it is split, and into how many chunks, follows from the number of tiles, on the device.)
 bool may_split(const Fp8GemmArgs& a, bool swiglu) {
     return a.K >= 16 * kFp8Block && expected_tiles(a, 256, swiglu ? 128 : 256) <= 8 * kSplitSlots;
 }
 
-// The 256 x 256 tiles where their rounds cost less than those of the ring's 64-row ones. A round of 256 of the former takes
-// about 2 us a block of K and 11 us besides, however many of the rows are real, a round of 512 of the latter 1.55 and 3 us.
-// (16 experts, 2048 -> 4096 -> 2048, the two products with the ring and with the large tiles: 66 + 44 us and 85 + 65 at 48
-// rows an expert, 82 + 53 and 85 + 67 at 64, 101 + 52 and 85 + 66 at 96, 150 + 78 and 84 + 67 at 128; 64 experts, 1024 -> 2048
-// -> 1024: 95 + 53 and 103 + 46 at 64 rows, 119 + 55 and 104 + 46 at 96.)
-bool use_pp(const Fp8GemmArgs& a, bool swiglu) {
+// Which tiles a product takes: those whose rounds are expected to take least time. A round is a workgroup a CU; two of the
+// ring's run together. Each takes a time per block of K and one at its end, fitted (us) to dense products of 512 to 4096 rows
+// and 1024 to 4096 wide:
+//   8-bit core, 64 rows: 0.50 n + 3.3 alone, 0.72 n + 4.5 the pair; 128 rows: 0.74 n + 3.6 and 1.07 n + 6.0;
+//   256 x 256: 1.59 n + 8.1, a split last round its share of the blocks, its end, and 6 + 0.055 a partial tile for the sums;
+//   exact, 64 rows: 0.73 n + 1.3 and 1.09 n + 3.8; 128 rows: 1.02 n + 2.5 and 1.78 n + 5.3.
+// Measured, 64 rows, 128 rows and 256 x 256 (8-bit core, whole call): one matrix 4096 x 4096 with 512 rows 25, 33, 43 us, 2048
+// rows 57, 45, 57, 4096 rows 112, 85, 64, 4400 rows 133, 107, 96, 512 rows of 14336 73, 93, 54; 8 groups 2048 -> 2048 of 100
+// rows 16, 20, 26, 400 rows 33, 25, 50, 600 rows 48, 41, 34; 64 groups 2048 -> 1408 of 32 rows 39, 42, 57, 100 rows 53, 47, 59,
+// 200 rows 86, 71, 83, 500 rows 221, 171, 133. Exact, 64 and 128 rows: one matrix with 512 rows 33, 42, 1024 rows 45, 45, 4096
+// rows 159, 129; 8 groups of 100 rows 19, 24, 400 rows 44, 36.
+struct RingCost {
+    double slab1, end1, slab2, end2;  // a workgroup alone, a pair
+};
+constexpr RingCost kRing64{0.50, 3.3, 0.72, 4.5}, kRing128{0.74, 3.6, 1.07, 6.0};
+constexpr RingCost kExact64{0.73, 1.3, 1.09, 3.8}, kExact128{1.02, 2.5, 1.78, 5.3};
+
+double ring_cost(const Fp8GemmArgs& a, int tm, int tn, const RingCost& c) {
     const double nkb = a.K / kFp8Block;
-    return offsets32(a) && nkb >= 2 &&
-           rounds(a, 256, swiglu ? 128 : 256, kSplitSlots) * (2.0 * nkb + 11.0) <=
-               rounds(a, 64, swiglu ? 64 : 128, 512) * (1.55 * nkb + 3.0);
+    // (an expected number barely past a round is as likely below it)
+    const int wgs = std::max(1, static_cast<int>(std::ceil(expected_tiles(a, tm, tn) / 256 - 0.02)));
+    return wgs / 2 * (c.slab2 * nkb + c.end2) + wgs % 2 * (c.slab1 * nkb + c.end1);
 }
 
-// Time of the ring's tiles of tm rows (us): two workgroups a CU, each of tm x 128 products, take 1.35 (64 rows) or 2.25 us
-// (128) a block of K together and 0.9 or 1.25 alone, and 3 us besides. The larger tile makes half the conversions a product and
-// wins from two rounds of the smaller on. Measured, 64 and 128 rows (float32 outputs): one matrix 4096 x 4096 with 512
-// rows 33 and 42, 1024 rows 45 and 45, 4096 rows 159 and 129; 8 groups 2048 -> 2048 of 100 rows 19 and 24, 200 rows 25 and 25, 400
-// rows 44 and 36; 64 groups 2048 -> 1408 of 32 rows 38 and 50, 100 rows 66 and 55, 128 rows 75 and 81, 500 rows 261 and 222.
-double ring_cost(const Fp8GemmArgs& a, int tm, int tn) {
-    const double nkb = a.K / kFp8Block;
-    const int halves = std::max(1, static_cast<int>(std::ceil(expected_tiles(a, tm, tn) / 256 - 0.1)));
-    return halves / 2 * ((tm == 64 ? 1.35 : 2.25) * nkb + 3.0) + halves % 2 * ((tm == 64 ? 0.9 : 1.25) * nkb + 3.0);
+double pp_cost(const Fp8GemmArgs& a, bool swiglu) {
+    const double nkb = a.K / kFp8Block, slab = 1.59, end = 8.1;
+    const double tiles = std::max(1.0, expected_tiles(a, 256, swiglu ? 128 : 256));
+    const double full = std::floor(tiles / kSplitSlots + 0.02), tail = tiles - full * kSplitSlots;
+    double t = full * (slab * nkb + end);
+    if (tail > 0.02 * kSplitSlots || full == 0) {
+        const int chunks = may_split(a, swiglu) ? std::max(1, static_cast<int>(std::min(kSplitSlots / tail, nkb / 2))) : 1;
+        t += slab * nkb / chunks + end + (chunks > 1 ? 6.0 + 0.055 * chunks * tail : 0.0);
+    }
+    return t;
 }
 
-template <typename TO, Epilogue EPI>
+bool use_pp(const Fp8GemmArgs& a, Epilogue epi) {
+    // (few rows are a stream of the weights, which the other kernels follow)
+    if (!offsets32(a) || a.K < 2 * kFp8Block || avg_rows(a) < 32) return false;
+    const bool swiglu = epi == Epilogue::SwiGLU;
+    const int tn = swiglu ? 64 : 128;
+    // hidden rows of the ring pass through memory in float32 and a launch of their own
+    const double extra = epi == Epilogue::Store ? 0.0 : 4.5 + static_cast<double>(a.rows) * a.N * 8 / 4.5e6;
+    return pp_cost(a, swiglu) <= extra + std::min(ring_cost(a, 64, tn, kRing64), ring_cost(a, 128, tn, kRing128));
+}
+
+template <typename TO, Epilogue EPI, bool EXACT>
 hipError_t dispatch_small(const Fp8GemmArgs& a, hipStream_t s) {
     const int tn = EPI == Epilogue::SwiGLU ? 64 : 128;
     if (!offsets32(a) || (avg_rows(a) < 32 && max_tiles(a, 32, tn) < 512)) return run_skinny<TO, 1, 1, 8, 4, EPI>(a, s);
-    if (avg_rows(a) < 16) return run_ring<TO, 32, 4, EPI, true>(a, s);
-    if (ring_cost(a, 128, tn) < ring_cost(a, 64, tn)) return run_ring<TO, 128, 2, EPI, false>(a, s);
-    return run_ring<TO, 64, 3, EPI, false>(a, s);
+    if (avg_rows(a) < 16) return run_ring<TO, 32, 4, EPI, true, true>(a, s);
+    if (ring_cost(a, 128, tn, EXACT ? kExact128 : kRing128) < ring_cost(a, 64, tn, EXACT ? kExact64 : kRing64))
+        return run_ring<TO, 128, 2, EPI, false, EXACT>(a, s);
+    return run_ring<TO, 64, 3, EPI, false, EXACT>(a, s);
 }
 
 }  // namespace
@@ -983,35 +1010,35 @@ bool fp8_gemm_fits(const Fp8GemmArgs& a) {
 
 hipError_t launch_fp8_gemm(DType out_type, const Fp8GemmArgs& a, hipStream_t s) {
     if (a.rows == 0) return hipSuccess;
-    if (out_type == DType::F32) return dispatch_small<float, Epilogue::Store>(a, s);
-    if (use_pp(a, false) && a.N % 8 == 0) return run_pp<Epilogue::Store>(a, s);
-    return dispatch_small<bf16_t, Epilogue::Store>(a, s);
+    if (out_type == DType::F32) return dispatch_small<float, Epilogue::Store, true>(a, s);
+    if (use_pp(a, Epilogue::Store) && a.N % 8 == 0) return run_pp<Epilogue::Store>(a, s);
+    return dispatch_small<bf16_t, Epilogue::Store, false>(a, s);
 }
 
-bool fp8_rows_half(const Fp8GemmArgs& a) { return use_pp(a, false); }
+bool fp8_rows_half(const Fp8GemmArgs& a) { return use_pp(a, Epilogue::Store); }
 
 hipError_t launch_fp8_rows(const Fp8GemmArgs& a, hipStream_t s) {
     if (a.rows == 0) return hipSuccess;
-    return fp8_rows_half(a) ? run_pp<Epilogue::Store, true>(a, s) : dispatch_small<float, Epilogue::Store>(a, s);
+    return fp8_rows_half(a) ? run_pp<Epilogue::Store, true>(a, s) : dispatch_small<float, Epilogue::Store, false>(a, s);
 }
 
 size_t fp8_split_scratch_bytes(Epilogue epi, const Fp8GemmArgs& a) {
     const bool swiglu = epi == Epilogue::SwiGLU;
-    return use_pp(a, swiglu) && may_split(a, swiglu) ? static_cast<size_t>(kSplitSlots) * 256 * 256 * sizeof(float) : 0;
+    return use_pp(a, epi) && may_split(a, swiglu) ? static_cast<size_t>(kSplitSlots) * 256 * 256 * sizeof(float) : 0;
 }
 
 size_t fp8_hidden_scratch_bytes(Epilogue epi, const Fp8GemmArgs& a) {
-    return use_pp(a, epi == Epilogue::SwiGLU) ? 0 : static_cast<size_t>(a.rows) * a.N * sizeof(float);
+    return use_pp(a, epi) ? 0 : static_cast<size_t>(a.rows) * a.N * sizeof(float);
 }
 
 hipError_t launch_fp8_hidden(Epilogue epi, const Fp8GemmArgs& a, float* scratch, hipStream_t s) {
     if (a.rows == 0) return hipSuccess;
     const bool swiglu = epi == Epilogue::SwiGLU;
-    if (use_pp(a, swiglu)) return swiglu ? run_pp<Epilogue::SwiGLU>(a, s) : run_pp<Epilogue::ReLU>(a, s);
+    if (use_pp(a, epi)) return swiglu ? run_pp<Epilogue::SwiGLU>(a, s) : run_pp<Epilogue::ReLU>(a, s);
     Fp8GemmArgs g = a;
     g.out = scratch;
-    const hipError_t e = swiglu ? dispatch_small<float, Epilogue::SwiGLU>(g, s)
-                                : dispatch_small<float, Epilogue::ReLU>(g, s);
+    const hipError_t e = swiglu ? dispatch_small<float, Epilogue::SwiGLU, false>(g, s)
+                                : dispatch_small<float, Epilogue::ReLU, false>(g, s);
     if (e != hipSuccess) return e;
     return launch_fp8_quantize(DType::F32, scratch, 1, static_cast<int>(a.rows), a.N, 1, a.out, a.out_scale, s);
 }

@@ -112,7 +112,10 @@ MATMULS = [
     # enough 256 x 256 tiles: whole rounds and less, ragged rows and columns, the last round split along K (an even and an
     # odd number of blocks, a chunk without any), widths that no 16-byte store fits
     (6144, 1, 2176, 384, 0), (5000, 3, 2184, 512, 7), (5000, 3, 2181, 512, 7), (3328, 1, 2304, 2048, 0),
-    (2200, 4, 2056, 2176, 100), (8448, 1, 2048, 2176, 0), (16640, 1, 1024, 256, 0),
+    (2200, 4, 2056, 2176, 100), (8448, 1, 2048, 2176, 0), (16640, 1, 1024, 256, 0), (8448, 1, 2048, 2048, 0),
+    (8700, 4, 2056, 4224, 100),
+    # 128-row tiles, groups of some hundred rows
+    (1024, 1, 4096, 1024, 0), (3000, 8, 1999, 1152, 41), (900, 8, 2048, 640, 0),
 ]
 
 
@@ -241,6 +244,11 @@ def _moe_reference(x, idx, w, w_in, w_down, act, dtype):
     (2600, 2, 1, 2, 2048, 1152, "swiglu", torch.bfloat16, 0.0),
     (2600, 2, 1, 2, 2048, 1152, "swiglu", torch.float32, 0.0),
     (2600, 2, 1, 2, 2176, 2432, "relu", torch.bfloat16, 0.0),
+    # output rows as float16 with scales, the last round split
+    (4300, 2, 2, 2, 2048, 2048, "swiglu", torch.bfloat16, 0.0),
+    # 64- and 128-row tiles of the hidden rows
+    (600, 8, 2, 8, 1024, 768, "swiglu", torch.bfloat16, 0.0),
+    (1000, 8, 2, 8, 640, 1024, "relu", torch.bfloat16, 0.3),
 ])
 def test_moe_forward_matches_the_oracle(T, M, k, keep, d, H, act, dtype, skew):
     say(f"fp8_moe_forward T={T} M={M} k={k} d={d} H={H} {act} {dtype}")
