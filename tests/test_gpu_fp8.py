@@ -158,6 +158,54 @@ def test_matmul_carries_nan_to_its_row_and_columns_only():
     assert (np.isnan(got) == want).all()
 
 
+@pytest.mark.parametrize("out_dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,G,n,k", [(1, 1, 300, 256), (600, 64, 256, 256), (512, 1, 1024, 512), (2048, 1, 4096, 512),
+                                        (4096, 1, 4096, 512)])
+def test_matmul_carries_nan_codes(rows, G, n, k, out_dtype):
+    """The code 0x7f (and 0xff) is NaN in the rows and the weights, in every kernel; codes next to it are numbers."""
+    say(f"fp8_matmul with NaN codes rows={rows} G={G} n={n} k={k} {out_dtype}")
+    a = torch.full((rows, k), 0x7e, dtype=torch.uint8, device=DEV)  # 448
+    b = torch.full((G, n, k), 0xfe, dtype=torch.uint8, device=DEV)  # -448
+    a[rows - 1, k - 1] = 0x7f
+    b[G - 1, 17, 3] = 0xff
+    seg = torch.arange(G + 1, device=DEV, dtype=torch.int32) * (rows // G)
+    seg[G] = rows
+    out = E.fp8_matmul(a.view(E.FP8), torch.ones((rows, k // 128), device=DEV), b.view(E.FP8),
+                       torch.ones((G, -(-n // 128), k // 128), device=DEV), seg, out_dtype=out_dtype)
+    want = torch.zeros((rows, n), dtype=torch.bool, device=DEV)
+    want[rows - 1] = True
+    want[int(seg[G - 1]):, 17] = True
+    assert torch.equal(torch.isnan(out), want)
+    assert (out[~want] == torch.tensor(-448.0 * 448.0 * k, dtype=out_dtype, device=DEV)).all()
+
+
+def test_matmul_captured_with_a_split_round():
+    """Replays of a product whose last round is split, between eager calls on the same workspace."""
+    rng = np.random.default_rng(16)
+    rows, n, k = 8448, 2048, 2048
+    b, b_s = E.fp8_quantize(up(rng.normal(size=(1, n, k)) * 0.02), 128)
+    xs = [E.fp8_quantize(up(rng.normal(size=(rows, k)))) for _ in range(2)]
+    desc = E.fp8_matmul_desc(rows, 1, n, k, torch.bfloat16)
+    need = E.fp8_matmul_workspace_size(desc)
+    assert need > 0
+    ws, out = E.workspace(need, DEV), torch.empty((rows, n), dtype=torch.bfloat16, device=DEV)
+    a, a_s = xs[0][0].clone(), xs[0][1].clone()
+    call = lambda: E.fp8_matmul_into(desc, a, a_s, None, b, b_s, out, ws)
+    refs = [E.fp8_matmul(*x, b[0], b_s[0]) for x in xs]
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for rep in range(4):
+        a.copy_(xs[rep % 2][0])
+        a_s.copy_(xs[rep % 2][1])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, refs[rep % 2]), f"replay {rep}"
+        assert torch.equal(E.fp8_matmul(*xs[1 - rep % 2], b[0], b_s[0], ws=ws), refs[1 - rep % 2])
+
+
 def test_matmul_with_no_rows_and_all_segments_empty():
     rng = np.random.default_rng(7)
     b, b_s, _ = quantised(rng, 3, 40, 128, 128)
