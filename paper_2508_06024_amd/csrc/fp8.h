@@ -37,8 +37,8 @@ struct Fp8GemmArgs {
 };
 // Whether a launch can hold the product's tiles, and 32 bits their offsets: larger ones are refused.
 bool fp8_gemm_fits(const Fp8GemmArgs& a);
-// out of out_type. Float32 outputs and small products: exact products (through bfloat16); large ones of bfloat16 outputs,
-// those of the 8-bit matrix core (fp8_device.h).
+// out of out_type. Float32 outputs and few rows a group: exact products (through bfloat16); else those of the 8-bit matrix
+// core (fp8_device.h).
 hipError_t launch_fp8_gemm(DType out_type, const Fp8GemmArgs& a, hipStream_t s);
 
 // Hidden rows of the experts: SwiGLU (weight rows 0..N-1 are the gate branch and N..2N-1 the up branch), silu(gate)
