@@ -686,9 +686,8 @@ ec2moe_status ec2moe_fp8_moe_forward(const ec2moe_moe_desc* desc, const void* x,
     Fp8Experts x8 = fp8_experts(desc, seg, perm_src);
     REQUIRE(fp8_gemm_fits(x8.in) && fp8_gemm_fits(x8.out), EC2MOE_ERR_UNSUPPORTED,
             "%lld assignments are too many for one launch", static_cast<long long>(A));
-    hipError_t e = launch_permute(topk_idx, A, desc->top_k, M, at<int32_t>(ws, w.counts), seg, perm_src, inv_perm,
-                                  stream);
-    if (e == hipSuccess) e = launch_fp8_quantize(dt, x, 1, T, d, 1, at<void>(ws, w.xq), at<float>(ws, w.xs), stream);
+    hipError_t e = launch_fp8_permute(topk_idx, A, desc->top_k, M, at<int32_t>(ws, w.counts), seg, perm_src, inv_perm, dt, x, T, d,
+                                      at<void>(ws, w.xq), at<float>(ws, w.xs), stream);
     if (e == hipSuccess) {
         Fp8GemmArgs& g = x8.in;
         g.a = at<uint8_t>(ws, w.xq); g.a_scale = at<float>(ws, w.xs); g.b = static_cast<const uint8_t*>(w_gate_up);

@@ -16,6 +16,11 @@ constexpr int kFp8Block = 128;  // values that share a scale
 hipError_t launch_fp8_quantize(DType dt, const void* x, int n_mats, int rows, int cols, int block_rows, void* q,
                                float* scale, hipStream_t s);
 
+// launch_permute and the quantisation of x [rows][cols] by rows, in one launch where the permutation takes one
+hipError_t launch_fp8_permute(const int32_t* topk_idx, int64_t n_assign, int top_k, int n_experts, int32_t* chunk_counts,
+                              int32_t* seg_offsets, int32_t* perm_src, int32_t* inv_perm, DType dt, const void* x, int rows,
+                              int cols, void* q, float* scale, hipStream_t s);
+
 // out[p][n] = sum_k a[row(p)][k] w_e[n][k] for every row p of group e on the scaled values, row(p) =
 // row_index ? row_index[p] : p.
 struct Fp8GemmArgs {

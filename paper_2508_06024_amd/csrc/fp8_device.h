@@ -52,6 +52,62 @@ __device__ __forceinline__ uint32_t quantize4(const float* x, const BlockScale& 
 
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
+// 8 consecutive values as loaded: one or two 16-byte chunks
+template <typename T>
+struct Eight {
+    static constexpr int kChunks = 8 / Elem<T>::kPerChunk;
+    uint4 c[kChunks];
+    __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) c[i] = ldg16(p + i * Elem<T>::kPerChunk);
+    }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) c[i] = make_uint4(0, 0, 0, 0);
+    }
+    __device__ __forceinline__ void values(float (&v)[8]) const {
+        const T* e = reinterpret_cast<const T*>(c);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = Elem<T>::to_f32(e[i]);
+    }
+};
+
+__device__ __forceinline__ uint32_t magnitude_max(const float (&v)[8]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+    return m;
+}
+
+// A scale per row and 128 columns: rows are whole blocks, so the blocks are consecutive runs of 128
+// values whatever the matrix. 16 lanes take a block, wave `w` of the launch U times four of them.
+template <typename T, int U>
+__device__ __forceinline__ void quantize_rows(const T* __restrict__ x, int64_t n_blocks, uint8_t* __restrict__ q,
+                                              float* __restrict__ scale, int64_t w) {
+    const int lane = threadIdx.x & 63;
+    const int64_t first = w * (4 * U) + (lane >> 4);
+    Eight<T> in[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t b = first + 4 * u;
+        if (b < n_blocks) in[u].load(x + b * kFp8Block + (lane & 15) * 8);
+        else in[u].clear();
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t b = first + 4 * u;
+        float v[8];
+        in[u].values(v);
+        uint32_t m = magnitude_max(v);
+#pragma unroll
+        for (int off = 1; off < 16; off <<= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), off)));
+        const BlockScale bs = block_scale(m);
+        if (b >= n_blocks) continue;
+        *reinterpret_cast<uint2*>(q + b * kFp8Block + (lane & 15) * 8) = make_uint2(quantize4(v, bs), quantize4(v + 4, bs));
+        if ((lane & 15) == 0) scale[b] = bs.scale;
+    }
+}
+
 // ------------------------------------------------------------------ float16 rows
 //
 // The power of two that brings values of magnitude up to `bits` into [2^14, 2^15), and its inverse: float16 then keeps

@@ -62,7 +62,7 @@ STAGE_OF_KERNEL = {
     "codec_z_bf16": "decode", "codec_prep": "decode", "codec_vzt": "decode", "codec_uw": "decode",
     "codec_decode": "decode",
     "expert_gate_up": "expert_gate_up", "expert_in_relu": "expert_in_relu", "expert_down": "expert_down",
-    "fp8_quantize_rows": "permute", "fp8_expert_gate_up": "expert_gate_up", "fp8_expert_in_relu": "expert_in_relu",
+    "fp8_permute_quantize": "permute", "fp8_quantize_rows": "permute", "fp8_expert_gate_up": "expert_gate_up", "fp8_expert_in_relu": "expert_in_relu",
     "fp8_expert_down": "expert_down", "fp8_combine": "combine",
     "combine": "combine",
 }
