@@ -294,6 +294,8 @@ def _moe_reference(x, idx, w, w_in, w_down, act, dtype):
     (2600, 2, 1, 2, 2176, 2432, "relu", torch.bfloat16, 0.0),
     # output rows as float16 with scales, the last round split
     (4300, 2, 2, 2, 2048, 2048, "swiglu", torch.bfloat16, 0.0),
+    # more assignments than one launch permutes
+    (9000, 16, 8, 16, 128, 128, "swiglu", torch.bfloat16, 0.0),
     # 64- and 128-row tiles of the hidden rows
     (600, 8, 2, 8, 1024, 768, "swiglu", torch.bfloat16, 0.0),
     (1000, 8, 2, 8, 640, 1024, "relu", torch.bfloat16, 0.3),
