@@ -110,16 +110,20 @@ __device__ __forceinline__ void quantize_rows(const T* __restrict__ x, int64_t n
 
 // ------------------------------------------------------------------ float16 rows
 //
-// The power of two that brings values of magnitude up to `bits` into [2^14, 2^15), and its inverse: float16 then keeps
-// 11 bits of the largest and of everything down to 2^-28 of it. With an infinity or NaN among them both are 1.
+// The power of two that brings values of magnitude up to `bits`, the largest finite one of the block, into [2^14, 2^15),
+// and its inverse: float16 then keeps 11 bits of the largest and of everything down to 2^-28 of it. Infinities and NaN
+// survive any such scale and have no part in the choice of it. 1 for a block without a finite value but zero.
 struct HalfScale {
     float scale, inv;
 };
 __device__ __forceinline__ HalfScale half_scale(uint32_t bits) {
-    const uint32_t e = bits >> 23;
-    if (e == 255) return {1.f, 1.f};
-    const uint32_t c = max(e, 15u);
+    if (bits == 0) return {1.f, 1.f};
+    const uint32_t c = max(bits >> 23, 15u);
     return {__uint_as_float((c - 14u) << 23), __uint_as_float((268u - c) << 23)};
+}
+__device__ __forceinline__ uint32_t finite_magnitude(float v) {
+    const uint32_t m = magnitude(v);
+    return m < 0x7f800000u ? m : 0u;
 }
 
 // ------------------------------------------------------------------ products of a block of 128

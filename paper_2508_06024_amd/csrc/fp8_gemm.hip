@@ -776,6 +776,13 @@ __global__ __launch_bounds__(512, 1) void fp8_pp_kernel(Fp8GemmArgs p) {
                 for (int ni = 0; ni < NI; ++ni)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) m = max(m, magnitude(acc[ni][mi][e]));
+                if (__any(m >= 0x7f800000u)) {  // rare: an infinity or a NaN in one of the wave's rows
+                    m = 0;
+#pragma unroll
+                    for (int ni = 0; ni < NI; ++ni)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) m = max(m, finite_magnitude(acc[ni][mi][e]));
+                }
                 m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 16)));
                 m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 32)));
                 hs = half_scale(m);
@@ -849,7 +856,7 @@ __global__ __launch_bounds__(256) void fp8_split_reduce_kernel(Fp8GemmArgs p) {
         if constexpr (HALF) {
             uint32_t m = 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) m = max(m, magnitude(v[e]));
+            for (int e = 0; e < 4; ++e) m = max(m, finite_magnitude(v[e]));
 #pragma unroll
             for (int off = 1; off < 32; off <<= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), off)));
             const HalfScale hs = half_scale(m);
