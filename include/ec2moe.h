@@ -352,8 +352,8 @@ ec2moe_status ec2moe_fp8_moe_workspace_size(const ec2moe_moe_desc* desc, size_t*
 /*
  * ec2moe_moe_forward with 8-bit expert weights: x is quantised by rows, the hidden activations
  * (silu(gate) * up, or relu(W_in x)) are quantised by rows from their float32 values, both products
- * are those of ec2moe_fp8_matmul (the hidden activations as with bfloat16 outputs), and the weighted sum of a token's rows is accumulated in float32 in
- * slot order from rows of 11 bits or more, and rounded once.
+ * are those of ec2moe_fp8_matmul with outputs of the descriptor's dtype, and the weighted sum of a
+ * token's rows is accumulated in float32 in slot order from rows of 11 bits or more, and rounded once.
  *   x [T][d], y [T][d] out in the descriptor's dtype; topk_idx, topk_w as in ec2moe_moe_forward
  *   (a slot whose id is outside [0, M), as of a padding token, adds nothing);
  *   w_gate_up [M][2H][d] (EC2MOE_EXPERT_RELU: [M][H][d]) with w_gate_up_scale [M][2H/128][d/128]

@@ -608,8 +608,9 @@ Fp8MoeWs fp8_moe_ws(const ec2moe_moe_desc* d) {
     const int64_t T = d->n_tokens, A = T * d->top_k, kb = d->d_model / kFp8Block, hb = d->ffn_hidden / kFp8Block;
     const int32_t some = 0;
     const Fp8Experts x = fp8_experts(d, &some, &some);
-    const size_t part_in = fp8_split_scratch_bytes(x.epi, x.in);
-    const size_t part_out = d->dtype == EC2MOE_F32 ? 0 : fp8_split_scratch_bytes(Epilogue::Store, x.out);
+    const bool exact = d->dtype == EC2MOE_F32;  // takes no split
+    const size_t part_in = exact ? 0 : fp8_split_scratch_bytes(x.epi, x.in);
+    const size_t part_out = exact ? 0 : fp8_split_scratch_bytes(Epilogue::Store, x.out);
     Fp8MoeWs w{};
     size_t o = 0;
     w.counts = o; o += up(static_cast<size_t>(std::max(1, perm_chunks(A))) * d->n_experts * 4);
@@ -618,10 +619,10 @@ Fp8MoeWs fp8_moe_ws(const ec2moe_moe_desc* d) {
     w.inv_perm = o; o += up(static_cast<size_t>(A) * 4);
     w.xq = o; o += up(static_cast<size_t>(T) * d->d_model);
     w.xs = o; o += up(static_cast<size_t>(T) * kb * 4);
-    w.act = o; o += up(fp8_hidden_scratch_bytes(x.epi, x.in));
+    w.act = o; o += up(fp8_hidden_scratch_bytes(x.epi, x.in, exact));
     w.act_q = o; o += up(static_cast<size_t>(A) * d->ffn_hidden);
     w.act_s = o; o += up(static_cast<size_t>(A) * hb * 4);
-    w.half = d->dtype == EC2MOE_BF16 && fp8_rows_half(x.out);
+    w.half = !exact && fp8_rows_half(x.out);
     w.y_perm = o; o += up(static_cast<size_t>(A) * d->d_model * (w.half ? 2 : 4));
     w.y_scale = o; o += up(w.half ? static_cast<size_t>(A) * kb * 4 : 0);
     w.part = o; o += up(std::max(part_in, part_out));
@@ -678,7 +679,7 @@ ec2moe_status ec2moe_fp8_moe_forward(const ec2moe_moe_desc* desc, const void* x,
     REQUIRE_ALIGNED(x); REQUIRE_ALIGNED(w_gate_up); REQUIRE_ALIGNED(w_gate_up_scale); REQUIRE_ALIGNED(w_down);
     REQUIRE_ALIGNED(w_down_scale); REQUIRE_ALIGNED(y);
     const DType dt = static_cast<DType>(desc->dtype);
-    const int T = desc->n_tokens, d = desc->d_model, H = desc->ffn_hidden, M = desc->n_experts;
+    const int T = desc->n_tokens, d = desc->d_model, M = desc->n_experts;
     const int64_t A = static_cast<int64_t>(T) * desc->top_k;
     int32_t* seg = at<int32_t>(ws, w.seg);
     int32_t* perm_src = at<int32_t>(ws, w.perm_src);
@@ -693,7 +694,7 @@ ec2moe_status ec2moe_fp8_moe_forward(const ec2moe_moe_desc* desc, const void* x,
         g.a = at<uint8_t>(ws, w.xq); g.a_scale = at<float>(ws, w.xs); g.b = static_cast<const uint8_t*>(w_gate_up);
         g.b_scale = w_gate_up_scale; g.out = at<void>(ws, w.act_q); g.out_scale = at<float>(ws, w.act_s);
         if (w.split_in) g.part = at<float>(ws, w.part);
-        e = launch_fp8_hidden(x8.epi, g, at<float>(ws, w.act), stream);
+        e = launch_fp8_hidden(x8.epi, g, dt == DType::F32, at<float>(ws, w.act), stream);
     }
     if (e == hipSuccess) {
         Fp8GemmArgs& g = x8.out;

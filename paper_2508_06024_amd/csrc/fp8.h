@@ -48,8 +48,9 @@ hipError_t launch_fp8_gemm(DType out_type, const Fp8GemmArgs& a, hipStream_t s);
 
 // Hidden rows of the experts: SwiGLU (weight rows 0..N-1 are the gate branch and N..2N-1 the up branch), silu(gate)
 // * up, or ReLU, max(sum, 0); N and K multiples of 128. Quantised by rows from their float32 values to out and
-// out_scale, by way of scratch (fp8_hidden_scratch_bytes) where the product's tiles do not hold whole blocks.
-hipError_t launch_fp8_hidden(Epilogue epi, const Fp8GemmArgs& a, float* scratch, hipStream_t s);
+// out_scale, by way of scratch (fp8_hidden_scratch_bytes) where the product's tiles do not hold whole blocks. exact: sums of
+// exact products for any number of rows, as of launch_fp8_gemm with float32 outputs.
+hipError_t launch_fp8_hidden(Epilogue epi, const Fp8GemmArgs& a, bool exact, float* scratch, hipStream_t s);
 
 // Rows for launch_fp8_combine (N a multiple of 128): float16 with a scale per 128 columns in out_scale where
 // fp8_rows_half(), else float32.
@@ -60,7 +61,7 @@ hipError_t launch_fp8_combine(const void* rows, const float* scale, const int32_
                               int top_k, int d, void* y, hipStream_t s);
 
 // Scratch of a product, from the shape fields of its arguments and whether they have seg and row_index.
-size_t fp8_hidden_scratch_bytes(Epilogue epi, const Fp8GemmArgs& a);
+size_t fp8_hidden_scratch_bytes(Epilogue epi, const Fp8GemmArgs& a, bool exact);
 size_t fp8_split_scratch_bytes(Epilogue epi, const Fp8GemmArgs& a);
 
 }  // namespace ec2moe

@@ -12,8 +12,9 @@
 //   * fp8_ring_kernel (32- to 128-row tiles): operands through a ring of LDS slabs;
 //   * fp8_pp_kernel (256 x 256 tiles, bfloat16 outputs and hidden rows): two groups of waves that alternate between
 //     products and memory.
-// The first, the ring's 32-row tiles and float32 outputs multiply exactly, through bfloat16 (with few rows a group memory is
-// the bound); the others use the 8-bit matrix core, at twice the rate, whose sums are cut off as fp8_device.h says.
+// The first, the ring's 32-row tiles, float32 outputs and a float32 layer's hidden rows multiply exactly, through bfloat16
+// (with few rows a group memory is the bound); the others use the 8-bit matrix core, at twice the rate, whose sums are cut
+// off as fp8_device.h says.
 //
 // Measured: one row of 4096 x 4096 weights 5.8 us (2.9 TB/s of weights, a launch's length); 32 tokens through 40 of 64
 // experts of 4096 -> 1536, 8 a token, 86 us (5.8 TB/s) and 50 (5.0); 8 experts of 4096 -> 14336, 8192 rows, 2.05
@@ -26,6 +27,7 @@
 
 #include <cmath>
 #include <string>
+#include <type_traits>
 
 namespace ec2moe {
 namespace {
@@ -1034,18 +1036,20 @@ size_t fp8_split_scratch_bytes(Epilogue epi, const Fp8GemmArgs& a) {
     return use_pp(a, epi) && may_split(a, swiglu) ? static_cast<size_t>(kSplitSlots) * 256 * 256 * sizeof(float) : 0;
 }
 
-size_t fp8_hidden_scratch_bytes(Epilogue epi, const Fp8GemmArgs& a) {
-    return use_pp(a, epi) ? 0 : static_cast<size_t>(a.rows) * a.N * sizeof(float);
+size_t fp8_hidden_scratch_bytes(Epilogue epi, const Fp8GemmArgs& a, bool exact) {
+    return !exact && use_pp(a, epi) ? 0 : static_cast<size_t>(a.rows) * a.N * sizeof(float);
 }
 
-hipError_t launch_fp8_hidden(Epilogue epi, const Fp8GemmArgs& a, float* scratch, hipStream_t s) {
+hipError_t launch_fp8_hidden(Epilogue epi, const Fp8GemmArgs& a, bool exact, float* scratch, hipStream_t s) {
     if (a.rows == 0) return hipSuccess;
     const bool swiglu = epi == Epilogue::SwiGLU;
-    if (use_pp(a, epi)) return swiglu ? run_pp<Epilogue::SwiGLU>(a, s) : run_pp<Epilogue::ReLU>(a, s);
+    if (!exact && use_pp(a, epi)) return swiglu ? run_pp<Epilogue::SwiGLU>(a, s) : run_pp<Epilogue::ReLU>(a, s);
     Fp8GemmArgs g = a;
     g.out = scratch;
-    const hipError_t e = swiglu ? dispatch_small<float, Epilogue::SwiGLU, false>(g, s)
-                                : dispatch_small<float, Epilogue::ReLU, false>(g, s);
+    auto go = [&](auto ex) {
+        return swiglu ? dispatch_small<float, Epilogue::SwiGLU, ex.value>(g, s) : dispatch_small<float, Epilogue::ReLU, ex.value>(g, s);
+    };
+    const hipError_t e = exact ? go(std::true_type{}) : go(std::false_type{});
     if (e != hipSuccess) return e;
     return launch_fp8_quantize(DType::F32, scratch, 1, static_cast<int>(a.rows), a.N, 1, a.out, a.out_scale, s);
 }

@@ -51,3 +51,60 @@ def test_columns_beside_one_that_is_not_finite_are_as_without_it(T, M, k, d, H, 
     keep[bad] = False
     assert torch.equal(got[:, keep], ref[:, keep])
     assert (torch.isnan(got[:, bad]) if kind == "nan" else got[:, bad] == float("inf")).all()
+
+
+# ----------------------------------------------------------------------------- sums of products of unequal size
+
+def _cancelling(rng, rows, k, sign, low, high):
+    """Rows of e4m3 values whose runs of 8 begin 448, sign 448 and go on with three small whole numbers and zeros: of a row
+    of either sign the first two products cancel, and the others lie up to 17 bits below them."""
+    v = rng.integers(low, high + 1, size=(rows, k // 8, 8)).astype(np.float64)
+    v[:, :, 0], v[:, :, 1] = 448.0, sign * 448.0
+    v[:, :, 5:] = 0
+    return v.reshape(rows, k)
+
+
+@pytest.mark.parametrize("act", ["relu", "swiglu"])
+@pytest.mark.parametrize("T,M,d,H", [(6, 2, 256, 256), (40, 64, 256, 1024), (600, 2, 256, 256), (9000, 4, 128, 512), (3000, 2, 2048, 1024)])
+def test_hidden_rows_of_a_float32_layer_are_sums_of_exact_products(T, M, d, H, act):
+    """Rows of scale 1 whose large products cancel: the hidden sums are whole numbers below 2^24, which float32 sums of exact
+    products give whatever their order. The output weights are identities (on 256 columns of H), so that the output is the
+    quantised hidden row itself."""
+    say(f"fp8_moe_forward float32 exact hidden rows T={T} M={M} d={d} H={H} {act}")
+    rng = np.random.default_rng(T + H)
+    n = min(d, H)
+    x = _cancelling(rng, T, d, 1.0, 1, 4)  # blocks' largest value 448: the scale is 1
+    rows = E.w_in_rows(H, act)
+    w = np.stack([_cancelling(rng, rows, d, -1.0, -3, 4) for _ in range(M)])
+    if act == "swiglu":
+        w[:, :H] = np.abs(w[:, :H])  # gates of 32 and more: silu(g) = g in float32
+        w[:, :H, 1::8] *= -1
+    w_dn = np.zeros((M, d, H))
+    w_dn[:, np.arange(n), np.arange(n)] = 1.0
+    ones = lambda *shape: torch.ones(shape, device=DEV)
+    idx = rng.integers(0, M, size=(T, 1)).astype(np.int32)
+    h = np.empty((T, rows))
+    for e in range(M):
+        own = idx[:, 0] == e
+        h[own] = x[own] @ w[e].T
+    h = np.maximum(h, 0) if act == "relu" else h[:, :H] * h[:, H:]
+    assert np.abs(h).max() < 2 ** 24 and (act == "relu" or np.abs(h).min(axis=1).max() > 0)
+    y = E.fp8_moe_forward(up(x), up(idx, torch.int32), ones(T, 1), up(w).to(E.FP8), ones(M, rows // 128, d // 128),
+                          up(w_dn).to(E.FP8), ones(M, d // 128, H // 128), activation=act)
+    q, s = E.fp8_quantize(up(h))
+    want = q.float() * s.repeat_interleave(128, dim=1)
+    assert torch.equal(y[:, :n], want[:, :n]) and (y[:, n:] == 0).all()
+
+
+@pytest.mark.parametrize("rows,G,n,k", [(3, 1, 300, 512), (300, 64, 1100, 384), (512, 1, 1024, 512), (4096, 1, 1024, 512),
+                                        (3000, 8, 1999, 256)])
+def test_float32_products_are_sums_of_exact_products(rows, G, n, k):
+    """As above for the product by itself: its sums are whole numbers, and exact."""
+    say(f"fp8_matmul float32 exact rows={rows} G={G} n={n} k={k}")
+    rng = np.random.default_rng(rows + n)
+    a, w = _cancelling(rng, rows, k, 1.0, 1, 15), np.stack([_cancelling(rng, n, k, -1.0, -15, 15) for _ in range(G)])
+    seg = (np.arange(G + 1) * rows // G).astype(np.int32)
+    got = E.fp8_matmul(up(a).to(E.FP8), torch.ones((rows, k // 128), device=DEV), up(w).to(E.FP8),
+                       torch.ones((G, -(-n // 128), k // 128), device=DEV), up(seg, torch.int32), out_dtype=torch.float32)
+    want = np.concatenate([a[seg[g]:seg[g + 1]] @ w[g].T for g in range(G)])
+    assert torch.equal(got, up(want))
