@@ -383,7 +383,8 @@ ec2moe_status ec2moe_balance_loss_workspace_size(const ec2moe_moe_desc* desc, si
  *   d_probs     [M] float32 out or NULL: coef * M * f_i / T', the gradient of the loss with
  *               respect to probs[t][i], the same for every valid token t: the d_balance of
  *               ec2moe_group_gate_backward
- * Indices outside [0, M) are not counted. d_model and ffn_hidden of the descriptor are not used.
+ * Indices outside [0, M) are not counted. d_model and ffn_hidden of the descriptor are not used and may
+ * hold anything; T * k < 2^31.
  */
 ec2moe_status ec2moe_balance_loss(const ec2moe_moe_desc* desc, const float* probs, const int32_t* topk_idx,
                                   const uint8_t* token_valid, float coef, int32_t* counts, float* loss,

@@ -69,13 +69,13 @@ constexpr int kMaxGateRows = 320;
 constexpr int kMaxTopK = 16;
 
 // equal_groups: K must divide M (the gate without group sizes; the entry points after the
-// gate never read the group structure)
-ec2moe_status check_moe_desc(const ec2moe_moe_desc* d, bool equal_groups = true) {
+// gate never read the group structure). widths: d_model and ffn_hidden are used.
+ec2moe_status check_moe_desc(const ec2moe_moe_desc* d, bool equal_groups = true, bool widths = true) {
     REQUIRE(d != nullptr, EC2MOE_ERR_INVALID_ARGUMENT, "desc is NULL");
     REQUIRE(d->dtype == EC2MOE_F32 || d->dtype == EC2MOE_BF16, EC2MOE_ERR_INVALID_ARGUMENT, "unknown dtype %d",
             static_cast<int>(d->dtype));
     REQUIRE(d->n_tokens >= 0, EC2MOE_ERR_INVALID_ARGUMENT, "n_tokens %d < 0", d->n_tokens);
-    REQUIRE(d->n_experts > 0 && d->n_groups > 0 && d->d_model > 0 && d->ffn_hidden > 0 && d->top_k > 0,
+    REQUIRE(d->n_experts > 0 && d->n_groups > 0 && (!widths || (d->d_model > 0 && d->ffn_hidden > 0)) && d->top_k > 0,
             EC2MOE_ERR_INVALID_ARGUMENT, "n_experts, n_groups, d_model, ffn_hidden and top_k must be positive");
     REQUIRE(!equal_groups || d->n_experts % d->n_groups == 0, EC2MOE_ERR_INVALID_ARGUMENT,
             "n_groups %d does not divide n_experts %d", d->n_groups, d->n_experts);
@@ -89,11 +89,16 @@ ec2moe_status check_moe_desc(const ec2moe_moe_desc* d, bool equal_groups = true)
     REQUIRE(d->n_experts + d->n_groups <= kMaxGateRows, EC2MOE_ERR_UNSUPPORTED, "n_experts + n_groups > %d",
             kMaxGateRows);
     REQUIRE(d->top_k <= kMaxTopK, EC2MOE_ERR_UNSUPPORTED, "top_k %d > %d", d->top_k, kMaxTopK);
+    const int64_t A = static_cast<int64_t>(d->n_tokens) * d->top_k;
+    if (!widths) {
+        REQUIRE(A < (int64_t(1) << 31), EC2MOE_ERR_UNSUPPORTED, "%d tokens top-%d: more assignments than 32-bit counts hold",
+                d->n_tokens, d->top_k);
+        return EC2MOE_OK;
+    }
     REQUIRE(d->d_model % 128 == 0, EC2MOE_ERR_UNSUPPORTED, "d_model %d is not a multiple of 128", d->d_model);
     REQUIRE(d->ffn_hidden % 128 == 0, EC2MOE_ERR_UNSUPPORTED, "ffn_hidden %d is not a multiple of 128",
             d->ffn_hidden);
     // 32-bit byte offsets inside one operand of the GEMM
-    const int64_t A = static_cast<int64_t>(d->n_tokens) * d->top_k;
     const int64_t eb = d->dtype == EC2MOE_F32 ? 4 : 2;
     REQUIRE(A * std::max(d->d_model, d->ffn_hidden) * eb < (int64_t(1) << 32) &&
                 int64_t(2) * d->ffn_hidden * d->d_model * eb < (int64_t(1) << 32),
@@ -713,7 +718,7 @@ ec2moe_status ec2moe_fp8_moe_forward(const ec2moe_moe_desc* desc, const void* x,
 // ---------------------------------------------------------------- training the router
 
 ec2moe_status ec2moe_balance_loss_workspace_size(const ec2moe_moe_desc* desc, size_t* bytes) {
-    if (ec2moe_status st = check_moe_desc(desc, false); st != EC2MOE_OK) return st;
+    if (ec2moe_status st = check_moe_desc(desc, false, false); st != EC2MOE_OK) return st;
     REQUIRE_PTR(bytes);
     *bytes = balance_ws_bytes(desc->n_tokens, desc->n_experts);
     return ok();
@@ -722,7 +727,7 @@ ec2moe_status ec2moe_balance_loss_workspace_size(const ec2moe_moe_desc* desc, si
 ec2moe_status ec2moe_balance_loss(const ec2moe_moe_desc* desc, const float* probs, const int32_t* topk_idx,
                                   const uint8_t* token_valid, float coef, int32_t* counts, float* loss,
                                   float* d_probs, void* ws, size_t ws_bytes, hipStream_t stream) {
-    if (ec2moe_status st = check_moe_desc(desc, false); st != EC2MOE_OK) return st;
+    if (ec2moe_status st = check_moe_desc(desc, false, false); st != EC2MOE_OK) return st;
     if (ec2moe_status st = check_ws(ws, ws_bytes, balance_ws_bytes(desc->n_tokens, desc->n_experts)); st != EC2MOE_OK)
         return st;
     REQUIRE_PTR(loss);

@@ -845,7 +845,7 @@ size_t balance_ws_bytes(int n_tokens, int n_experts) {
 
 hipError_t launch_balance(const BalanceArgs& a, hipStream_t s) {
     const int chunks0 = balance_chunks(a.n_tokens, a.n_experts);
-    const int chunk = std::max(1, (a.n_tokens + chunks0 - 1) / chunks0);
+    const int chunk = std::max(1, static_cast<int>((static_cast<int64_t>(a.n_tokens) + chunks0 - 1) / chunks0));
     const int chunks = chunks0;  // trailing ones may be empty
     {
         ProfileScope prof(kBalanceName, s);

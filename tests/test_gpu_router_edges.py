@@ -1,0 +1,36 @@
+"""The router's training operators at sizes where they can go wrong, on the GPU."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2508_06024_amd import ec2moe as E
+from tests.gpu_common import say
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+
+
+# ----------------------------------------------------------------------------- balance loss
+
+def test_balance_loss_of_a_batch_longer_than_a_layer_of_it():
+    """18 million tokens, with a descriptor of a wide layer."""
+    say("balance_loss of 18 million tokens")
+    T, M = 18_000_001, 2
+    g = torch.Generator(device=DEV)
+    g.manual_seed(3)
+    p = torch.rand((T, M), device=DEV, generator=g)
+    idx = (torch.rand((T, 1), device=DEV, generator=g) < 0.3).int()
+    desc = E.moe_desc(T, M, 1, 4096, 14336, 1, torch.bfloat16)
+    ws = E.workspace(E.balance_loss_workspace_size(desc), DEV)
+    loss, d = torch.empty(1, device=DEV), torch.empty(M, device=DEV)
+    counts = torch.empty(M, dtype=torch.int32, device=DEV)
+    E.balance_loss_into(desc, p, idx, 0.5, loss, counts, d, ws)
+    ones = int(idx.sum())
+    assert counts.tolist() == [T - ones, ones]
+    f = np.array([T - ones, ones]) / T
+    mean = p.double().sum(dim=0).cpu().numpy() / T
+    # float32 sums of some 400 positive terms (138 rows a thread, then 256 threads), the rest in float64
+    assert abs(float(loss) / (0.5 * M * (f * mean).sum()) - 1) <= 512 * 2.0 ** -24
+    np.testing.assert_allclose(d.double().cpu().numpy(), 0.5 * M * f / T, rtol=3 * 2.0 ** -24)
+    assert all(torch.equal(a, b) for a, b in zip((loss, counts, d), E.balance_loss(p, idx, 0.5)))
