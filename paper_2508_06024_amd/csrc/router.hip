@@ -25,6 +25,7 @@ constexpr const char *kBalanceName = "balance_loss", *kBalanceFinishName = "bala
 // short ones are two launches.
 constexpr int kBalThreads = 512;
 constexpr int kBalMaxChunks = 512;
+constexpr int kBalRows = 8;   // rows of a float32 sum, loaded together
 constexpr int kBalCols = 32;  // experts of a workgroup of the second launch
 
 int balance_chunks(int n_tokens, int n_experts) {
@@ -60,7 +61,7 @@ __device__ __forceinline__ double balance_expert(const BalanceArgs& a, int e, do
 // V: consecutive experts a thread loads together
 template <int V>
 __global__ __launch_bounds__(kBalThreads) void balance_kernel(BalanceArgs a, int chunk) {
-    __shared__ float s_sum[kBalThreads * V];
+    __shared__ double s_sum[kBalThreads * V];
     __shared__ int s_cnt[kMaxExperts];
     __shared__ int s_n;
     __shared__ double s_loss[kMaxExperts];
@@ -76,25 +77,37 @@ __global__ __launch_bounds__(kBalThreads) void balance_kernel(BalanceArgs a, int
     if (tid == 0) s_n = 0;
     __syncthreads();
     const int rs = tid / L, c = (tid % L) * V;
-    float sum[V];
+    double sum[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) sum[v] = 0.f;
+    for (int v = 0; v < V; ++v) sum[v] = 0.0;
     if (rs < RP) {
-        // (a token that does not count adds zero, not its value times zero)
-#pragma unroll 8
-        for (int t = rs; t < nt; t += RP) {
+        // Eight rows are summed in float32, these sums in float64, so that the error does not grow with the batch. (A token
+        // that does not count adds zero, not its value times zero.)
+        auto add = [&](int t, float (&run)[V]) {
             const bool ok = !valid || valid[t];
             if constexpr (V == 4) {
                 const f32x4 v = *reinterpret_cast<const f32x4*>(probs + static_cast<int64_t>(t) * M + c);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sum[i] += ok ? v[i] : 0.f;
+                for (int i = 0; i < 4; ++i) run[i] += ok ? v[i] : 0.f;
             } else {
                 const float v = probs[static_cast<int64_t>(t) * M + c];
-                sum[0] += ok ? v : 0.f;
+                run[0] += ok ? v : 0.f;
             }
+        };
+        int t = rs;
+        for (; t + (kBalRows - 1) * RP < nt; t += kBalRows * RP) {
+            float run[V] = {};
+#pragma unroll
+            for (int u = 0; u < kBalRows; ++u) add(t + u * RP, run);
+#pragma unroll
+            for (int v = 0; v < V; ++v) sum[v] += run[v];
         }
+        float run[V] = {};
+        for (; t < nt; t += RP) add(t, run);
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum[v] += run[v];
     }
-    // a thread keeps its slot of the token: 256 / k tokens a pass
+    // a thread keeps its slot of the token: kBalThreads / k tokens a pass
     const int tp = kBalThreads / k, slot = tid % k;
 #pragma unroll 4
     for (int t = tid / k; t < nt; t += tp) {
@@ -113,9 +126,16 @@ __global__ __launch_bounds__(kBalThreads) void balance_kernel(BalanceArgs a, int
 #pragma unroll
         for (int v = 0; v < V; ++v) s_sum[rs * L * V + c + v] = sum[v];
     __syncthreads();
-    float p = 0.f;
-    if (tid < M)
-        for (int r = 0; r < RP; ++r) p += s_sum[r * L * V + tid];
+    double p = 0.0;
+    if (tid < M) {
+        double q[4] = {0.0, 0.0, 0.0, 0.0};  // four sums side by side: a float64 addition's latency each
+        int r = 0;
+        for (; r + 4 <= RP; r += 4)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) q[u] += s_sum[(r + u) * L * V + tid];
+        for (; r < RP; ++r) q[0] += s_sum[r * L * V + tid];
+        p = (q[0] + q[1]) + (q[2] + q[3]);
+    }
     if (gridDim.x == 1) {
         if (tid < M) s_loss[tid] = balance_expert(a, tid, p, s_cnt[tid], s_n);
         __syncthreads();
@@ -128,7 +148,7 @@ __global__ __launch_bounds__(kBalThreads) void balance_kernel(BalanceArgs a, int
     }
     const BalancePart part = balance_part(a.ws, gridDim.x, M);
     if (tid < M) {
-        part.p[static_cast<int64_t>(blockIdx.x) * M + tid] = p;
+        part.p[static_cast<int64_t>(blockIdx.x) * M + tid] = static_cast<float>(p);  // half the traffic of the second launch
         part.c[static_cast<int64_t>(blockIdx.x) * M + tid] = s_cnt[tid];
     }
     if (tid == 0) {

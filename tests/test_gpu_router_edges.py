@@ -34,3 +34,16 @@ def test_balance_loss_of_a_batch_longer_than_a_layer_of_it():
     assert abs(float(loss) / (0.5 * M * (f * mean).sum()) - 1) <= 512 * 2.0 ** -24
     np.testing.assert_allclose(d.double().cpu().numpy(), 0.5 * M * f / T, rtol=3 * 2.0 ** -24)
     assert all(torch.equal(a, b) for a, b in zip((loss, counts, d), E.balance_loss(p, idx, 0.5)))
+
+
+@pytest.mark.parametrize("T,M,value", [(2_000_003, 250, 0.1), (1_000_001, 256, 0.7), (9_000_000, 7, 0.013), (300, 8, 0.3)])
+def test_balance_loss_of_long_batches_keeps_float32_precision(T, M, value):
+    """Equal probabilities, whose float32 sums in a row would drift one way."""
+    say(f"balance_loss of equal probabilities T={T} M={M}")
+    p = torch.full((T, M), value, device=DEV)
+    idx = (torch.arange(T, device=DEV, dtype=torch.int32) % M).reshape(T, 1)
+    loss, counts, _ = E.balance_loss(p, idx, 1.0)
+    f = np.bincount(np.arange(T) % M, minlength=M) / T
+    assert counts.tolist() == np.bincount(np.arange(T) % M, minlength=M).tolist()
+    # sums of 8 float32 terms (7 roundings), a chunk's sum and the loss rounded once each; the rest in float64
+    assert abs(float(loss) / (M * float(np.float32(value)) * f.sum()) - 1) <= 10 * 2.0 ** -24
