@@ -211,6 +211,16 @@ def gate_opts(top_groups: int = 0, group_sizes: Optional[Sequence[int]] = None, 
     return opts
 
 
+def _opts_ref(desc: MoeDesc, opts: Optional[GateOpts]):
+    """The options by reference. The library reads a size for each group of the descriptor."""
+    if opts is None:
+        return None
+    sizes = getattr(opts, "_sizes", None)
+    if sizes is not None and len(sizes) != desc.n_groups:
+        raise ValueError(f"group_sizes has {len(sizes)} sizes for {desc.n_groups} groups")
+    return ctypes.byref(opts)
+
+
 def gate_workspace_size(desc: MoeDesc) -> int:
     n = ctypes.c_size_t(0)
     _check(_lib.ec2moe_gate_workspace_size(ctypes.byref(desc), ctypes.byref(n)))
@@ -220,7 +230,7 @@ def gate_workspace_size(desc: MoeDesc) -> int:
 def group_gate_ex(desc: MoeDesc, opts: Optional[GateOpts], mask_words, x, w_global, b_global, w_local, b_local,
                   topk_idx, topk_w, probs=None):
     """Raw call with options (top-G groups, unequal group sizes)."""
-    _check(_lib.ec2moe_group_gate_ex(ctypes.byref(desc), ctypes.byref(opts) if opts is not None else None,
+    _check(_lib.ec2moe_group_gate_ex(ctypes.byref(desc), _opts_ref(desc, opts),
                                      mask_array(mask_words), _ptr(x), _ptr(w_global), _ptr(b_global),
                                      _ptr(w_local), _ptr(b_local), _ptr(topk_idx), _ptr(topk_w), _ptr(probs),
                                      _stream()))
@@ -546,7 +556,7 @@ def group_gate_backward_into(desc: MoeDesc, opts: Optional[GateOpts], x, w_globa
     """Raw call with caller-owned outputs (None: not computed) and workspace."""
     addr = lambda t: None if t is None else t.data_ptr()
     grads = GateGrads(addr(d_topk_w), addr(d_probs), addr(d_balance), addr(token_valid))
-    _check(_lib.ec2moe_group_gate_backward(ctypes.byref(desc), ctypes.byref(opts) if opts is not None else None,
+    _check(_lib.ec2moe_group_gate_backward(ctypes.byref(desc), _opts_ref(desc, opts),
                                            ctypes.byref(grads), _ptr(x), _ptr(w_global), _ptr(w_local), _ptr(probs),
                                            _ptr(topk_idx), _ptr(d_x), _ptr(d_w_global), _ptr(d_b_global), _ptr(d_w_local),
                                            _ptr(d_b_local), _ptr(ws), ws.numel(), _stream()))

@@ -27,3 +27,16 @@ def _balance_size(**kw):
 ])
 def test_balance_loss_does_not_use_the_layer_widths(kw, status):
     assert _balance_size(**kw) == status, E.last_error()
+
+
+@pytest.mark.parametrize("sizes", [[8], [3, 3, 2], [1] * 8, []])
+def test_group_sizes_of_another_number_of_groups_are_refused(sizes):
+    """The library reads one size for each group of the descriptor."""
+    import torch
+    desc = E.moe_desc(4, 8, 2, 128, 128, 2, E.BF16)
+    t = torch.zeros(16)
+    opts = E.gate_opts(0, sizes)
+    with pytest.raises(ValueError, match="group_sizes"):
+        E.group_gate_backward_into(desc, opts, t, t, t, t, t, t)
+    with pytest.raises(ValueError, match="group_sizes"):
+        E.group_gate_ex(desc, opts, [0xff], t, t, None, t, None, t, t)
