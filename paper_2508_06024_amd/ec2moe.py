@@ -176,6 +176,9 @@ def moe_desc(n_tokens, n_experts, n_groups, d_model, ffn_hidden, top_k, dtype, r
     if activation not in ACTIVATIONS:
         raise ValueError(f"activation must be one of {ACTIVATIONS}, got {activation!r}")
     flags = (GATE_RENORMALIZE if renormalize else 0) | (EXPERT_RELU if activation == "relu" else 0)
+    for v in (n_tokens, n_experts, n_groups, d_model, ffn_hidden, top_k):
+        if not -2 ** 31 <= v < 2 ** 31:
+            raise ValueError(f"size {v} does not fit the descriptor's 32 bits")
     return MoeDesc(n_tokens=n_tokens, d_model=d_model, n_experts=n_experts, n_groups=n_groups, top_k=top_k,
                    ffn_hidden=ffn_hidden, dtype=dtype if isinstance(dtype, int) else dtype_code(dtype), flags=flags)
 

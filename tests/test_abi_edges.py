@@ -40,3 +40,11 @@ def test_group_sizes_of_another_number_of_groups_are_refused(sizes):
         E.group_gate_backward_into(desc, opts, t, t, t, t, t, t)
     with pytest.raises(ValueError, match="group_sizes"):
         E.group_gate_ex(desc, opts, [0xff], t, t, None, t, None, t, t)
+
+
+def test_moe_desc_refuses_sizes_beyond_32_bits():
+    """A field of the descriptor is an int32: more tokens would be taken as their remainder."""
+    for n in (2 ** 31, 2 ** 32, 2 ** 32 + 64, -2 ** 31 - 1):
+        with pytest.raises(ValueError):
+            E.moe_desc(n, 8, 2, 128, 256, 2, E.BF16)
+    assert E.moe_desc(2 ** 31 - 1, 8, 2, 128, 256, 2, E.BF16).n_tokens == 2 ** 31 - 1
