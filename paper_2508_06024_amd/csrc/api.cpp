@@ -8,6 +8,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -537,7 +538,7 @@ ec2moe_status ec2moe_fp8_quantize(const void* x, ec2moe_dtype x_dtype, int32_t n
     REQUIRE(cols % kFp8Block == 0, EC2MOE_ERR_UNSUPPORTED, "cols %d is not a multiple of %d", cols, kFp8Block);
     // a launch of fewer than 2^32 threads: a workgroup per 64 row blocks, or per 128 x 128 block
     const double groups = static_cast<double>(n_mats) * (cols / kFp8Block) *
-                          (block_rows == 1 ? rows / 64.0 : (rows + kFp8Block - 1) / kFp8Block);
+                          (block_rows == 1 ? rows / 64.0 : std::ceil(static_cast<double>(rows) / kFp8Block));
     REQUIRE(groups < 16.0e6, EC2MOE_ERR_UNSUPPORTED, "%d x %d x %d values are too many for one launch", n_mats, rows,
             cols);
     if (n_mats == 0 || rows == 0) return ok();

@@ -48,3 +48,12 @@ def test_moe_desc_refuses_sizes_beyond_32_bits():
         with pytest.raises(ValueError):
             E.moe_desc(n, 8, 2, 128, 256, 2, E.BF16)
     assert E.moe_desc(2 ** 31 - 1, 8, 2, 128, 256, 2, E.BF16).n_tokens == 2 ** 31 - 1
+
+
+@pytest.mark.parametrize("rows,block_rows,status", [
+    (2 ** 31 - 1, 128, UNSUPPORTED), (2 ** 31 - 128, 128, UNSUPPORTED), (2 ** 31 - 1, 1, UNSUPPORTED),
+    (2 ** 31 - 1, 2, INVALID),
+])
+def test_quantize_refuses_more_rows_than_a_launch_takes(rows, block_rows, status):
+    p = ctypes.c_void_p(1 << 20)
+    assert E._lib.ec2moe_fp8_quantize(p, E.BF16, 1, rows, 128, block_rows, p, p, None) == status, E.last_error()
