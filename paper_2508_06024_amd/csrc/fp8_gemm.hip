@@ -26,7 +26,7 @@
 #include "gemm_tiles.h"
 
 #include <cmath>
-#include <string>
+#include <cstdio>
 #include <type_traits>
 
 namespace ec2moe {
@@ -926,8 +926,9 @@ hipError_t run_pp(const Fp8GemmArgs& a, hipStream_t s) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.part) return e;
     // a tail is split into two chunks or more: at most half a round of tiles
-    const std::string name = std::string(a.name) + "_tail";
-    ProfileScope prof(name.c_str(), s);
+    char name[48];  // of the timing record; no allocation, which could throw
+    std::snprintf(name, sizeof name, "%s_tail", a.name);
+    ProfileScope prof(name, s);
     hipLaunchKernelGGL((fp8_split_reduce_kernel<EPI, HALF>), dim3(kSplitSlots / 2 * 16), dim3(256), 0, s, a);
     return hipGetLastError();
 }
