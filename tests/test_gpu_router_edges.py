@@ -5,6 +5,7 @@ import torch
 
 from paper_2508_06024_amd import ec2moe as E
 from tests.gpu_common import say
+from tests.test_gpu_router import test_gate_backward_matches_the_oracle as _matches_the_oracle
 
 pytestmark = pytest.mark.gpu
 
@@ -47,3 +48,17 @@ def test_balance_loss_of_long_batches_keeps_float32_precision(T, M, value):
     assert counts.tolist() == np.bincount(np.arange(T) % M, minlength=M).tolist()
     # sums of 8 float32 terms (7 roundings), a chunk's sum and the loss rounded once each; the rest in float64
     assert abs(float(loss) / (M * float(np.float32(value)) * f.sum()) - 1) <= 10 * 2.0 ** -24
+
+
+# ----------------------------------------------------------------------------- gate backward
+
+@pytest.mark.parametrize("T,d,M,K,k,keep,renorm,terms,pad,dtype", [
+    (70, 128, 64, 1, 6, 64, True, "wb", 0.0, torch.float32),       # one group of a whole wave
+    (65, 256, 256, 4, 8, 200, False, "wpb", 0.2, torch.bfloat16),  # groups of 64
+    (41, 128, 128, 1, 4, 100, True, "wb", 0.0, torch.bfloat16),    # one group of more than 64
+    (130, 128, 256, 1, 16, 256, True, "wpb", 0.0, torch.float32),
+    (4099, 128, 192, 2, 8, 150, True, "wb", 0.1, torch.bfloat16),  # groups of 96, more than a token a wave
+    (50, 128, 100, 4, 3, 80, False, "wb", 0.0, torch.bfloat16),    # groups of 25
+])
+def test_gate_backward_of_groups_of_any_size(T, d, M, K, k, keep, renorm, terms, pad, dtype):
+    _matches_the_oracle(T, d, M, K, k, keep, False, renorm, terms, pad, dtype)
