@@ -81,22 +81,22 @@ __device__ __forceinline__ void spread(float v, float (&out)[MI]) {
 
 // ------------------------------------------------------------------ few rows
 //
-// A tile of 16 MT token rows and 16 NT weight rows (SwiGLU: NT gate and NT up blocks) by WAVES waves that
-// take every WAVES-th block of K, fragments straight from memory; their sums meet in LDS and are added
-// in wave order.
-template <typename TO, int MT, int NT, int WAVES, int U, Epilogue EPI>
-__global__ __launch_bounds__(64 * WAVES) void fp8_skinny_kernel(Fp8GemmArgs p) {
+// A tile of 16 token rows and 16 output columns (SwiGLU: their gate and up rows) by kFewWaves waves that take every
+// kFewWaves-th block of K, fragments straight from memory, kFewDepth blocks of each in flight; their sums meet in LDS and
+// are added in wave order.
+constexpr int kFewWaves = 8, kFewDepth = 4;
+template <typename TO, Epilogue EPI>
+__global__ __launch_bounds__(64 * kFewWaves) void fp8_skinny_kernel(Fp8GemmArgs p) {
     constexpr bool SWIGLU = EPI == Epilogue::SwiGLU;
-    constexpr int NB = SWIGLU ? 2 * NT : NT;  // weight blocks
-    constexpr int TM = 16 * MT, TN = 16 * NT;
-    __shared__ f32x4 red[WAVES][NB * MT][64];
+    constexpr int NB = SWIGLU ? 2 : 1;  // weight blocks of 16 rows
+    __shared__ f32x4 red[kFewWaves][NB][64];
     TileInfo ti;
-    const int ntn = (p.N + TN - 1) / TN;
-    if (!find_tile<TM>(p, ntn, ti)) return;
+    const int ntn = (p.N + 15) / 16;
+    if (!find_tile<16>(p, ntn, ti)) return;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const int l16 = lane & 15, lg = lane >> 4;
     const int nkb = p.K / kFp8Block;
-    const int n0 = ti.nt * TN;
+    const int n0 = ti.nt * 16;
 
     const uint8_t* wrow[NB];
     const float* wscale[NB];
@@ -104,91 +104,70 @@ __global__ __launch_bounds__(64 * WAVES) void fp8_skinny_kernel(Fp8GemmArgs p) {
     const float* sg = p.b_scale + static_cast<int64_t>(ti.group) * scale_rows(p) * nkb;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-        const int r0 = SWIGLU && nb >= NT ? p.N + n0 + (nb - NT) * 16 : n0 + nb * 16;
+        const int r0 = nb * p.N + n0;
         const int last = p.b_rows - 1;
         wrow[nb] = wg + static_cast<int64_t>(min(r0 + l16, last)) * p.K + lg * 16;
         wscale[nb] = sg + static_cast<int64_t>(min(r0, last) / kFp8Block) * nkb;
     }
-    const uint8_t* trow[MT];
-    const float* tscale[MT];
+    const int64_t pos = ti.row0 + min(l16, ti.valid - 1);
+    const int64_t src = p.row_index ? p.row_index[pos] : pos;
+    const uint8_t* trow = p.a + src * p.K + lg * 16;
+    const float* tscale = p.a_scale + src * nkb;
+    f32x4 acc[NB];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-        const int64_t pos = ti.row0 + min(mt * 16 + l16, ti.valid - 1);
-        const int64_t src = p.row_index ? p.row_index[pos] : pos;
-        trow[mt] = p.a + src * p.K + lg * 16;
-        tscale[mt] = p.a_scale + src * nkb;
-    }
-    f32x4 acc[NB][MT];
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) acc[nb][mt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int nb = 0; nb < NB; ++nb) acc[nb] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    // U blocks of K in flight; those past the end repeat the last one and count zero
-    for (int kb0 = wave; kb0 < nkb; kb0 += WAVES * U) {
-        i32x8 fw[U][NB], ft[U][MT];
-        float sw[U][NB], st[U][MT];
+    // blocks past the end repeat the last one and are not counted
+    for (int kb0 = wave; kb0 < nkb; kb0 += kFewWaves * kFewDepth) {
+        i32x8 fw[kFewDepth][NB], ft[kFewDepth];
+        float sw[kFewDepth][NB], st[kFewDepth];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int kb = min(kb0 + u * WAVES, nkb - 1);
+        for (int u = 0; u < kFewDepth; ++u) {
+            const int kb = min(kb0 + u * kFewWaves, nkb - 1);
             const int64_t off = static_cast<int64_t>(kb) * kFp8Block;
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
                 fw[u][nb] = frag8(ldg16_nt(wrow[nb] + off), ldg16_nt(wrow[nb] + off + 64));
                 sw[u][nb] = wscale[nb][kb];
             }
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                ft[u][mt] = frag8(ldg16(trow[mt] + off), ldg16(trow[mt] + off + 64));
-                st[u][mt] = tscale[mt][kb];
-            }
+            ft[u] = frag8(ldg16(trow + off), ldg16(trow + off + 64));
+            st[u] = tscale[kb];
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (kb0 + u * WAVES >= nkb) break;  // uniform
-            Wide wt[MT];
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) wt[mt] = widen(ft[u][mt]);
+        for (int u = 0; u < kFewDepth; ++u) {
+            if (kb0 + u * kFewWaves >= nkb) break;  // uniform
+            const Wide wt = widen(ft[u]);
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
-                const Wide ww = widen(fw[u][nb]);
+                const f32x4 part = mfma_wide(widen(fw[u][nb]), wt);
+                const float s = sw[u][nb] * st[u];
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    const f32x4 part = mfma_wide(ww, wt[mt]);
-                    const float s = sw[u][nb] * st[u][mt];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[nb][mt][i] = fmaf(part[i], s, acc[nb][mt][i]);
-                }
+                for (int i = 0; i < 4; ++i) acc[nb][i] = fmaf(part[i], s, acc[nb][i]);
             }
         }
     }
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) red[wave][nb * MT + mt][lane] = acc[nb][mt];
+    for (int nb = 0; nb < NB; ++nb) red[wave][nb][lane] = acc[nb];
     __syncthreads();
-    auto total = [&](int blk) {
-        f32x4 v = red[0][blk][lane];
+    if (wave > 0) return;
+    auto total = [&](int nb) {
+        f32x4 v = red[0][nb][lane];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) v += red[w][blk][lane];
+        for (int w = 1; w < kFewWaves; ++w) v += red[w][nb][lane];
         return v;
     };
-    TO* out = static_cast<TO*>(p.out);
-    for (int blk = wave; blk < NT * MT; blk += WAVES) {
-        const int nb = blk / MT, mt = blk % MT;
-        f32x4 v = total(blk);
-        if constexpr (SWIGLU) {
-            const f32x4 u = total(NT * MT + blk);
+    f32x4 v = total(0);
+    if constexpr (SWIGLU) {
+        const f32x4 u = total(1);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = silu(v[i]) * u[i];
-        } else if constexpr (EPI == Epilogue::ReLU) {
+        for (int i = 0; i < 4; ++i) v[i] = silu(v[i]) * u[i];
+    } else if constexpr (EPI == Epilogue::ReLU) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = relu(v[i]);
-        }
-        const int r = mt * 16 + l16, c = n0 + nb * 16 + 4 * lg;
-        if (r < ti.valid && c < p.N)
-            store_run(out + (ti.row0 + r) * p.N + c, v, p.N - c, c + 4 <= p.N && p.N % 4 == 0);
+        for (int i = 0; i < 4; ++i) v[i] = relu(v[i]);
     }
+    const int c = n0 + 4 * lg;
+    if (l16 < ti.valid && c < p.N)
+        store_run(static_cast<TO*>(p.out) + (ti.row0 + l16) * p.N + c, v, p.N - c, c + 4 <= p.N && p.N % 4 == 0);
 }
 
 // Weight row (within the group's matrix) of tile row n: SwiGLU tiles hold TN/2 gate rows, then the matching up
@@ -901,11 +880,10 @@ unsigned tile_grid(const Fp8GemmArgs& a, int tm, int tn) {
     return static_cast<unsigned>((max_tiles(a, tm, tn) + kXcds - 1) / kXcds * kXcds);
 }
 
-template <typename TO, int MT, int NT, int WAVES, int U, Epilogue EPI>
+template <typename TO, Epilogue EPI>
 hipError_t run_skinny(const Fp8GemmArgs& a, hipStream_t s) {
     ProfileScope prof(a.name, s);
-    hipLaunchKernelGGL((fp8_skinny_kernel<TO, MT, NT, WAVES, U, EPI>), dim3(tile_grid(a, 16 * MT, 16 * NT)), dim3(64 * WAVES), 0,
-                       s, a);
+    hipLaunchKernelGGL((fp8_skinny_kernel<TO, EPI>), dim3(tile_grid(a, 16, 16)), dim3(64 * kFewWaves), 0, s, a);
     return hipGetLastError();
 }
 
@@ -1002,7 +980,7 @@ bool use_pp(const Fp8GemmArgs& a, Epilogue epi) {
 template <typename TO, Epilogue EPI, bool EXACT>
 hipError_t dispatch_small(const Fp8GemmArgs& a, hipStream_t s) {
     const int tn = EPI == Epilogue::SwiGLU ? 64 : 128;
-    if (!offsets32(a) || (avg_rows(a) < 32 && max_tiles(a, 32, tn) < 512)) return run_skinny<TO, 1, 1, 8, 4, EPI>(a, s);
+    if (!offsets32(a) || (avg_rows(a) < 32 && max_tiles(a, 32, tn) < 512)) return run_skinny<TO, EPI>(a, s);
     if (avg_rows(a) < 16) return run_ring<TO, 32, 4, EPI, true, true>(a, s);
     if (ring_cost(a, 128, tn, EXACT ? kExact128 : kRing128) < ring_cost(a, 64, tn, EXACT ? kExact64 : kRing64))
         return run_ring<TO, 128, 2, EPI, false, EXACT>(a, s);

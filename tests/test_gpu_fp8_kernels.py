@@ -57,7 +57,7 @@ def reference(a, w, seg, out):
     (700, 64, 1102, 640, 7, "fp8_ring<{t},32,4,Store,true,true>"),
     (90, 200, 777, 1152, 0, "fp8_ring<{t},32,4,Store,true,true>"),
     # few tiles
-    (60, 16, 300, 640, 3, "fp8_skinny<{t},1,1,8,4,Store>"),
+    (60, 16, 300, 640, 3, "fp8_skinny<{t},Store>"),
 ])
 def test_products_of_few_rows_a_group(rows, G, n, k, tail, kernel, out_dtype):
     say(f"fp8_matmul few rows={rows} G={G} n={n} k={k} {out_dtype}")
@@ -93,7 +93,7 @@ def test_nan_codes_in_products_of_few_rows_a_group(out_dtype):
 
 
 @pytest.mark.parametrize("rows,n,k,out_dtype,kernel", [
-    (40, 260, 512, torch.bfloat16, "fp8_skinny<bf16,1,1,8,4,Store>"),
+    (40, 260, 512, torch.bfloat16, "fp8_skinny<bf16,Store>"),
     (300, 260, 512, torch.bfloat16, "fp8_ring<bf16,64,3,Store,false,false>"),
     (900, 2048, 640, torch.float32, "fp8_ring<float,64,3,Store,false,true>"),
     (2400, 2048, 640, torch.bfloat16, "fp8_ring<bf16,128,2,Store,false,false>"),
@@ -148,7 +148,7 @@ def test_products_of_operands_with_outliers(rows, n, k, out_dtype, kernel):
     (32, 64, 8, 1024, 512, "swiglu", torch.bfloat16, ["fp8_ring<float,32,4,SwiGLU,true,true>", "fp8_ring<float,32,4,Store,true,true>"]),
     (32, 64, 8, 1152, 1024, "relu", torch.bfloat16, ["fp8_ring<float,32,4,ReLU,true,true>", "fp8_ring<float,32,4,Store,true,true>"]),
     (40, 64, 8, 1152, 1024, "relu", torch.float32, ["fp8_ring<float,32,4,ReLU,true,true>", "fp8_ring<float,32,4,Store,true,true>"]),
-    (32, 64, 8, 640, 512, "swiglu", torch.float32, ["fp8_ring<float,32,4,SwiGLU,true,true>", "fp8_skinny<float,1,1,8,4,Store>"]),
+    (32, 64, 8, 640, 512, "swiglu", torch.float32, ["fp8_ring<float,32,4,SwiGLU,true,true>", "fp8_skinny<float,Store>"]),
     # hidden rows of the 256 x 256 tiles whose last round is split, K of an even and an odd number of blocks; the first two
     # leave float16 rows, from split sums too
     (4300, 2, 2, 2048, 2048, "swiglu", torch.bfloat16, ["fp8_pp<SwiGLU,false>", "fp8_split_reduce<SwiGLU,false>", "fp8_pp<Store,true>",
