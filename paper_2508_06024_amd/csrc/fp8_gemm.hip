@@ -926,7 +926,11 @@ double expected_tiles(const Fp8GemmArgs& a, int tm, int tn) {
     return mt * ((a.N + tn - 1) / tn);
 }
 // Whether the last round of the 256 x 256 tiles may be worth splitting along K: long K, and rounds few enough that it weighs.
-// (Whether it is split, and into how many chunks, follows from the number of tiles, on the device.)
+// (Whether it is split, and into how many chunks, follows from the number of tiles, on the device.) Measured, whole and split
+// (us): one matrix 2048 wide with 8448 rows, K 1024 36 and 40, 1536 47 and 47, 2048 58 and 54, 4096 99 and 86; 4096 wide with
+// 8448 rows, 2.1 rounds, K 2048 85 and 85, 4096 153 and 148, with 4400 rows and K 2048 55 and 63 (the sums of a round's eighth);
+// 8192 wide with 16640 rows, 8.1 rounds, K 2048 291 and 301, 4096 523 and 515; 17 rounds 524 and 525; without a part of a
+// round, 8 groups of 1056 rows, K 2048, 157 and 166 (the launch that finds no sums).
 bool may_split(const Fp8GemmArgs& a, bool swiglu) {
     return a.K >= 16 * kFp8Block && expected_tiles(a, 256, swiglu ? 128 : 256) <= 8 * kSplitSlots;
 }
@@ -968,7 +972,8 @@ double pp_cost(const Fp8GemmArgs& a, bool swiglu) {
 }
 
 bool use_pp(const Fp8GemmArgs& a, Epilogue epi) {
-    // (few rows are a stream of the weights, which the other kernels follow)
+    // Few rows are a stream of the weights, which the other kernels follow: 64 groups of 24 rows, 2048 -> 2048, 71 us here and
+    // 49 in the ring, 48 rows 74 and 61; 16 groups of 24 rows, 4096 -> 4096, 75 and 62.
     if (!offsets32(a) || a.K < 2 * kFp8Block || avg_rows(a) < 32) return false;
     const bool swiglu = epi == Epilogue::SwiGLU;
     const int tn = swiglu ? 64 : 128;
@@ -977,10 +982,20 @@ bool use_pp(const Fp8GemmArgs& a, Epilogue epi) {
     return pp_cost(a, swiglu) <= extra + std::min(ring_cost(a, 64, tn, kRing64), ring_cost(a, 128, tn, kRing128));
 }
 
+// The smaller tiles. Measured (us; few-row kernel, ring of 32, 64 and 128 rows):
+//   fewer than 32 rows a group and fewer 32-row tiles than CUs: the few-row kernel, whose 16 x 16 tiles are eight times as
+//   many. 1 row, 4096 -> 4096 (32 tiles), 7.0, 27, 22, -; 2 groups of 8 rows, 14336 -> 4096 (64), 34, 88, 92, -; 4 groups of 4,
+//   4096 -> 4096 (128), 19, 30, 31, -; 8 groups of 4, 2048 -> 2048 (144), 11, 16, 13, -; behind the limit 16 rows, 2048 -> 32768
+//   (256), 25, 18, 19, -; 8 groups of 4, 2048 -> 4096 (288), 19, 18, 19, -; 64 groups of 2, 2048 -> 1024 (544), 34, 24, 27, -.
+//   fewer than 16 rows a group: the ring of 32, a stream of weights with exact products. 64 groups, 2048 -> 2048, of 8 rows 68,
+//   46, 54, 56, of 24 rows 156, 49, 57, 60, of 48 rows 230, 85, 61, 64; with Zipf's lengths a mean of 8 rows 79, 43, 49, 51, 16
+//   rows 119, 58, 63, 60, 28 rows 169, 68, 66, 69; 1024 -> 4096, 16 rows 149, 63, 66, 66, 24 rows 192, 75, 68, 73; 16 groups,
+//   4096 -> 4096, 12 rows 97, 83, 69, 71. Equal lengths favour it up to 32 rows, unequal ones up to 12 to 24.
+//   else 64 or 128 rows by their cost.
 template <typename TO, Epilogue EPI, bool EXACT>
 hipError_t dispatch_small(const Fp8GemmArgs& a, hipStream_t s) {
     const int tn = EPI == Epilogue::SwiGLU ? 64 : 128;
-    if (!offsets32(a) || (avg_rows(a) < 32 && max_tiles(a, 32, tn) < 512)) return run_skinny<TO, EPI>(a, s);
+    if (!offsets32(a) || (avg_rows(a) < 32 && max_tiles(a, 32, tn) < 256)) return run_skinny<TO, EPI>(a, s);
     if (avg_rows(a) < 16) return run_ring<TO, 32, 4, EPI, true, true>(a, s);
     if (ring_cost(a, 128, tn, EXACT ? kExact128 : kRing128) < ring_cost(a, 64, tn, EXACT ? kExact64 : kRing64))
         return run_ring<TO, 128, 2, EPI, false, EXACT>(a, s);

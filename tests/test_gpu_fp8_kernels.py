@@ -56,8 +56,10 @@ def reference(a, w, seg, out):
     (290, 64, 1100, 512, 0, "fp8_ring<{t},32,4,Store,true,true>"),
     (700, 64, 1102, 640, 7, "fp8_ring<{t},32,4,Store,true,true>"),
     (90, 200, 777, 1152, 0, "fp8_ring<{t},32,4,Store,true,true>"),
-    # few tiles
+    (32, 8, 4100, 256, 0, "fp8_ring<{t},32,4,Store,true,true>"),
+    # fewer tiles than CUs
     (60, 16, 300, 640, 3, "fp8_skinny<{t},Store>"),
+    (31, 1, 4099, 1152, 0, "fp8_skinny<{t},Store>"),
 ])
 def test_products_of_few_rows_a_group(rows, G, n, k, tail, kernel, out_dtype):
     say(f"fp8_matmul few rows={rows} G={G} n={n} k={k} {out_dtype}")
@@ -148,7 +150,7 @@ def test_products_of_operands_with_outliers(rows, n, k, out_dtype, kernel):
     (32, 64, 8, 1024, 512, "swiglu", torch.bfloat16, ["fp8_ring<float,32,4,SwiGLU,true,true>", "fp8_ring<float,32,4,Store,true,true>"]),
     (32, 64, 8, 1152, 1024, "relu", torch.bfloat16, ["fp8_ring<float,32,4,ReLU,true,true>", "fp8_ring<float,32,4,Store,true,true>"]),
     (40, 64, 8, 1152, 1024, "relu", torch.float32, ["fp8_ring<float,32,4,ReLU,true,true>", "fp8_ring<float,32,4,Store,true,true>"]),
-    (32, 64, 8, 640, 512, "swiglu", torch.float32, ["fp8_ring<float,32,4,SwiGLU,true,true>", "fp8_skinny<float,Store>"]),
+    (32, 64, 8, 256, 512, "swiglu", torch.float32, ["fp8_ring<float,32,4,SwiGLU,true,true>", "fp8_skinny<float,Store>"]),
     # hidden rows of the 256 x 256 tiles whose last round is split, K of an even and an odd number of blocks; the first two
     # leave float16 rows, from split sums too
     (4300, 2, 2, 2048, 2048, "swiglu", torch.bfloat16, ["fp8_pp<SwiGLU,false>", "fp8_split_reduce<SwiGLU,false>", "fp8_pp<Store,true>",
