@@ -399,6 +399,11 @@ def _dev_here(t: torch.Tensor, name: str, dtype=None, shape=None):
     return t
 
 
+def _workspace_here(ws, nbytes: int, device):
+    """The caller's workspace, on the current device, or a new one."""
+    return workspace(nbytes, device) if ws is None else _dev_here(ws, "ws")
+
+
 def _blocks(n: int) -> int:
     return -(-n // FP8_BLOCK)
 
@@ -461,7 +466,7 @@ def fp8_matmul(a, a_scale, b, b_scale, seg_offsets=None, out_dtype=torch.bfloat1
         out = new((rows, n), dtype=out_dtype, device=a.device)
     _dev_here(out, "out", None, (rows, n))
     desc = fp8_matmul_desc(rows, G, n, k, out.dtype)
-    ws = ws if ws is not None else workspace(fp8_matmul_workspace_size(desc), a.device)
+    ws = _workspace_here(ws, fp8_matmul_workspace_size(desc), a.device)
     fp8_matmul_into(desc, a, a_scale, seg_offsets, bs, ss, out, ws)
     return out
 
@@ -501,7 +506,7 @@ def fp8_moe_forward(x, topk_idx, topk_w, w_gate_up, w_gate_up_scale, w_down, w_d
     _dev_here(topk_w, "topk_w", torch.float32, (T, k))
     M, H = _check_fp8_experts(w_gate_up, w_gate_up_scale, w_down, w_down_scale, d, activation)
     desc = moe_desc(T, M, 1, d, H, k, dt, activation=activation)
-    ws = ws if ws is not None else workspace(fp8_moe_workspace_size(desc), x.device)
+    ws = _workspace_here(ws, fp8_moe_workspace_size(desc), x.device)
     y = torch.empty((T, d), dtype=dt, device=x.device)
     fp8_moe_forward_into(desc, x, topk_idx, topk_w, w_gate_up, w_gate_up_scale, w_down, w_down_scale, y, ws)
     return y
@@ -539,7 +544,7 @@ def balance_loss(probs, topk_idx, coef=1.0, token_valid=None, ws=None):
     _dev_here(probs, "probs", torch.float32)
     _dev_here(topk_idx, "topk_idx", torch.int32, (T, k))
     desc = moe_desc(T, M, 1, FP8_BLOCK, FP8_BLOCK, k, BF16)
-    ws = ws if ws is not None else workspace(balance_loss_workspace_size(desc), probs.device)
+    ws = _workspace_here(ws, balance_loss_workspace_size(desc), probs.device)
     loss = torch.empty((1,), dtype=torch.float32, device=probs.device)
     counts = torch.empty((M,), dtype=torch.int32, device=probs.device)
     d_probs = torch.empty((M,), dtype=torch.float32, device=probs.device)
@@ -584,7 +589,7 @@ def group_gate_backward(x, w_global, w_local, probs, topk_idx, d_topk_w=None, d_
         if t is not None:
             _dev_here(t, name, torch.float32, shape)
     desc = moe_desc(T, M, K, d, FP8_BLOCK, k, dt, renormalize)
-    ws = ws if ws is not None else workspace(gate_backward_workspace_size(desc), x.device)
+    ws = _workspace_here(ws, gate_backward_workspace_size(desc), x.device)
     new = lambda *shape: torch.empty(shape, dtype=torch.float32, device=x.device)
     d_x = torch.empty_like(x) if with_dx else None
     d_wg, d_bg, d_wl, d_bl = new(K, d), new(K), new(M, d), new(M)

@@ -108,3 +108,18 @@ def test_float32_products_are_sums_of_exact_products(rows, G, n, k):
                        torch.ones((G, -(-n // 128), k // 128), device=DEV), up(seg, torch.int32), out_dtype=torch.float32)
     want = np.concatenate([a[seg[g]:seg[g + 1]] @ w[g].T for g in range(G)])
     assert torch.equal(got, up(want))
+
+
+# ----------------------------------------------------------------------------- workspaces
+
+@pytest.mark.parametrize("make", [lambda n: torch.empty(n, dtype=torch.uint8), lambda n: torch.empty((n, 2), dtype=torch.uint8, device=DEV)[:, 0]])
+def test_workspaces_on_the_host_or_with_gaps_are_refused(make):
+    ws, x = make(1 << 22), torch.zeros((64, 128), device=DEV)
+    q, s = E.fp8_quantize(x)
+    (wi, si), (wd, sd) = E.fp8_quantize(torch.zeros((2, 256, 128), device=DEV), 128), E.fp8_quantize(torch.zeros((2, 128, 128), device=DEV), 128)
+    idx, w = torch.zeros((64, 1), dtype=torch.int32, device=DEV), torch.ones((64, 1), device=DEV)
+    probs, gate = torch.full((64, 2), 0.5, device=DEV), torch.zeros((2, 128), device=DEV)
+    for call in (lambda: E.fp8_matmul(q, s, wi[0], si[0], ws=ws), lambda: E.fp8_moe_forward(x, idx, w, wi, si, wd, sd, ws=ws),
+                 lambda: E.balance_loss(probs, idx, ws=ws), lambda: E.group_gate_backward(x, gate, gate, probs, idx, ws=ws)):
+        with pytest.raises(ValueError, match="ws"):
+            call()
