@@ -22,6 +22,8 @@
  *     n_experts <= 256, n_experts + n_groups <= 320, n_groups <= n_experts (and
  *     dividing it for the gate without group sizes; the calls after the gate never
  *     read the group structure);
+ *     n_tokens * top_k * max(d_model, ffn_hidden) and 2 * d_model * ffn_hidden elements of the
+ *     dtype below 2^32 bytes (every call but ec2moe_balance_loss);
  *     codec ranks r_h, r_w multiples of 16 and at most 256, w a multiple of 128.
  *     Others return EC2MOE_ERR_UNSUPPORTED. n_tokens == 0 is valid and launches nothing.
  */
@@ -309,9 +311,9 @@ ec2moe_status ec2moe_lowrank_fit(const ec2moe_codec_desc* desc, const void* x, c
  * each) and scale. block_rows 1: a scale per row and 128 columns, scale [n_mats][rows][cols/128].
  * block_rows 128: a scale per 128 x 128 block of a matrix (the last block of rows may be
  * short), scale [n_mats][ceil(rows/128)][cols/128].
- * Per block: amax = max(max |x|, 2^-100), scale = amax / 448, q = e4m3(448 x / amax), the quotient
- * rounded once to float32 and then to the nearest 8-bit value (ties to even). A block that holds a
- * NaN or an infinity becomes NaN throughout.
+ * Per block: amax = max(max |x|, 2^-100), scale = amax / 448, q = e4m3(448 x / amax), the product and
+ * the quotient rounded to float32 (448 x is exact for bfloat16) and then to the nearest 8-bit value
+ * (ties to even). A block that holds a NaN or an infinity becomes NaN throughout.
  *   cols a positive multiple of 128; rows, n_mats >= 0 (0: nothing is launched).
  */
 ec2moe_status ec2moe_fp8_quantize(const void* x, ec2moe_dtype x_dtype, int32_t n_mats, int32_t rows, int32_t cols,
@@ -331,16 +333,18 @@ ec2moe_status ec2moe_fp8_matmul_workspace_size(const ec2moe_fp8_matmul_desc* des
 
 /*
  * out[p][c] = sum_j a[p][j] b_e[c][j] for every row p of segment e, on the numbers that the
- * 8-bit values and scales stand for. A block of 128 products is summed, multiplied by its two
- * scales and added to a float32 sum, which is rounded once to out_dtype. Within a block, float32
- * outputs, and bfloat16 ones of few rows a segment, sum exact products in float32. The others use
- * the 8-bit matrix core, which sums runs of 8 products in fixed point, cut off 13 bits below the
- * largest of the run, and the runs in float32.
+ * 8-bit values and scales stand for. A block of 128 products is summed, multiplied by the product
+ * of its two scales (a float32, which has to be in range) and added to a float32 sum, which is
+ * rounded once to out_dtype. Within a block, float32 outputs, and bfloat16 ones of few rows a
+ * segment, sum exact products in float32. The others use the 8-bit matrix core, which sums runs of
+ * 8 products in fixed point, cut off 13 bits below the largest of the run, and the runs in float32.
  *   a [rows][k], a_scale [rows][k/128]; b [n_groups][n][k], b_scale [n_groups][ceil(n/128)][k/128]
  *   seg_offsets [n_groups+1] int32: group e owns rows [seg[e], seg[e+1]), 0 = seg[0] <= ... <=
  *   seg[n_groups] <= rows, as from ec2moe_permute; NULL with n_groups == 1: every row.
  *   out [rows][n]; rows at or behind seg[n_groups] are left as they were.
- *   ws of ec2moe_fp8_matmul_workspace_size bytes. n * k < 2^32, k < 2^24; rows * n up to 2^34.
+ *   ws of ec2moe_fp8_matmul_workspace_size bytes. n * k < 2^32, k < 2^24 and
+ *   (rows / 32 + n_groups) * ceil(n / 64) < 2^24 - 8; from rows * k = 2^37 on, also
+ *   (rows / 16 + n_groups) * ceil(n / 16) < 2^23 - 8.
  */
 ec2moe_status ec2moe_fp8_matmul(const ec2moe_fp8_matmul_desc* desc, const void* a, const float* a_scale,
                                 const int32_t* seg_offsets, const void* b, const float* b_scale, void* out, void* ws,
@@ -354,6 +358,9 @@ ec2moe_status ec2moe_fp8_moe_workspace_size(const ec2moe_moe_desc* desc, size_t*
  * (silu(gate) * up, or relu(W_in x)) are quantised by rows from their float32 values, both products
  * are those of ec2moe_fp8_matmul with outputs of the descriptor's dtype, and the weighted sum of a
  * token's rows is accumulated in float32 in slot order from rows of 11 bits or more, and rounded once.
+ * In a bfloat16 layer the hidden sums of many rows an expert come from the 8-bit matrix core; values
+ * near a rounding border then take the neighbouring 8-bit step, so that a token's output differs by
+ * 2e-3 to 3e-3 of its norm with the number of tokens in the call (1.7e-3 is its own rounding).
  *   x [T][d], y [T][d] out in the descriptor's dtype; topk_idx, topk_w as in ec2moe_moe_forward
  *   (a slot whose id is outside [0, M), as of a padding token, adds nothing);
  *   w_gate_up [M][2H][d] (EC2MOE_EXPERT_RELU: [M][H][d]) with w_gate_up_scale [M][2H/128][d/128]

