@@ -707,8 +707,8 @@ __device__ __forceinline__ void gate_dw(const GateBackwardArgs& a, const uint16_
 }
 
 // Both products in one launch: the first dw_blocks workgroups of each of the dw_groups row groups d_W, the rest d_x. They
-// wait for memory at different times: 37 -> 28 us for 8192 tokens of 2048, 72 logits (67 MB of X and d_x; 4.7 MB of planes, which every
-// column tile reads from the L2s).
+// wait for memory at different times: 37 -> 31 us for 8192 tokens of 2048, 72 logits, 28 in long runs (67 MB of X and d_x; 4.7 MB of
+// planes, which every column tile reads from the L2s).
 struct GateProducts {
     const uint16_t* D;
     int ldd, chunk, chunks, dw_blocks, dw_groups;
